@@ -57,7 +57,8 @@ typedef enum {
     EC_ERR_WORKSPACE = 5,   /* workspace missing or smaller than *_workspace_bytes() */
     EC_ERR_UNSUPPORTED = 6, /* valid request outside what the kernels implement */
     EC_ERR_CUDA = 7,        /* a CUDA runtime call or launch failed */
-    EC_ERR_TIMEOUT = 8      /* (dev_status only) a bounded device-side wait gave up */
+    EC_ERR_TIMEOUT = 8,     /* (dev_status only) a bounded device-side wait gave up */
+    EC_ERR_PAGE = 9         /* (dev_status only) a page id outside the pool, or no free pages left */
 } ec_status;
 
 typedef enum { EC_F32 = 0, EC_BF16 = 1 } ec_dtype;
@@ -283,6 +284,173 @@ ec_status ec_select_recent_sliding(int32_t *history, int32_t ctx_len, int32_t ba
                                    uint8_t *masked, const uint8_t *decoded_flags, int32_t window,
                                    const int32_t *decision, int32_t k, int32_t *active_idx, int32_t n_cap,
                                    void *stream);
+
+/* ---- Paged cache ------------------------------------------------------------------------------------------------
+ * (The paper keeps one dense cache per batch; from here on a serving program's form of it: ragged sequences over pages
+ * that sequences may share.)
+ *
+ * k_pages, v_pages  [n_pages, n_kv_heads, page_size, head_dim]: a page holds page_size consecutive positions
+ * page_table        int32 [batch, max_pages]: position p of sequence b stands in page page_table[b, p / page_size]
+ * row_offsets       int32 [batch + 1], ascending: the new rows of sequence b are rows row_offsets[b] ..
+ *                   row_offsets[b+1] - 1 of q, k, v and out, all [n_rows, heads, head_dim]; rows behind
+ *                   row_offsets[batch] are padding: not read, left as they were
+ * kv_lens           int32 [batch]: positions of the sequence, its new rows among them
+ * All DEVICE pointers, read by the kernels: nothing about lengths is known on the host, so a captured call serves
+ * every later step. */
+typedef struct {
+    int32_t batch;       /* sequences, 1 .. EC_PAGED_MAX_BATCH */
+    int32_t n_q_heads;   /* H_q */
+    int32_t n_kv_heads;  /* H_kv; H_q % H_kv == 0 */
+    int32_t head_dim;    /* 64 or 128 */
+    int32_t dtype;       /* ec_dtype of q, the pages and out */
+    int32_t page_size;   /* positions of a page: 16, 32, 64 or 128 */
+    int32_t n_pages;     /* pages of the pool */
+    int32_t max_pages;   /* entries of a sequence in the page table */
+    int32_t mask_block;  /* which keys a row sees, see ec_attend_paged */
+    float   scale;       /* softmax scale; 0 means 1/sqrt(head_dim) */
+    uint32_t flags;      /* 0 */
+} ec_paged_desc;
+
+#define EC_PAGED_MAX_BATCH 1024
+
+/* Bytes of workspace ec_attend_paged needs (0 on bad arguments). */
+size_t ec_attend_paged_workspace_bytes(const ec_paged_desc *desc, int32_t max_rows);
+
+/* Attention of a chunk of new rows over the pages.  Row i (0-based) of the n_b rows of sequence b stands at position
+ * p = kv_lens[b] - n_b + i and sees the keys j < lim:
+ *     mask_block = 0:  lim = kv_lens[b]                                          (bidirectional, as ec_attend)
+ *     mask_block = m:  lim = min(kv_lens[b], (p / m + 1) * m)  for p >= 0, else 0  (m = 1: causal; m > 1: rows of a
+ *                      block of m positions see the whole block and what stands before it)
+ *     out[r, hq, :] = sum_{j < lim} softmax_j( scale * <q[r, hq, :], K[b, hq/g, j, :]> ) * V[b, hq/g, j, :]
+ * A row that sees nothing gets zeros.  What the pages hold at positions from kv_lens[b] on is never used, NaN and
+ * infinities there included; at the positions before it K and V must be finite.  fp32 accumulation, one rounding.
+ * n_rows: rows of q and out; max_rows: a bound of the rows of any one sequence (>= 1).  A sequence with more has only
+ * its first max_rows rows computed, and one with kv_lens[b] outside [0, max_pages * page_size] is cut to that range;
+ * both set *dev_status to EC_ERR_SHAPE.  A page id outside [0, n_pages) that a row would read sets it to EC_ERR_PAGE
+ * (nothing outside the pool is read).  *dev_status != 0 leaves `out` unspecified for that sequence (EC_ERR_TIMEOUT:
+ * for the call).  out may not overlap q.  workspace: at least ec_attend_paged_workspace_bytes() bytes, 16-byte aligned;
+ * nothing in it is kept between calls.  H_q / H_kv is limited to 128 (EC_ERR_UNSUPPORTED beyond). */
+ec_status ec_attend_paged(const ec_paged_desc *desc, const void *q, const int32_t *row_offsets, const int32_t *kv_lens,
+                          int32_t n_rows, int32_t max_rows, const int32_t *page_table, const void *k_pages,
+                          const void *v_pages, void *out, void *workspace, size_t workspace_bytes,
+                          int32_t *dev_status, void *stream);
+
+/* Host-only: which kernel ec_attend_paged picks ("" on bad arguments); the string is static. */
+const char *ec_attend_paged_kernel_name(const ec_paged_desc *desc, int32_t max_rows);
+
+/* ---- Norms of queries and keys, and the position rotation -------------------------------------------------------- */
+#define EC_ROPE_INTERLEAVED 1u   /* pairs are columns (2i, 2i+1); without it (i, i + rot_dim/2) */
+
+typedef struct {
+    int32_t n_q_heads, n_kv_heads;
+    int32_t head_dim;    /* 64 or 128 */
+    int32_t dtype;       /* ec_dtype of q, k, v, the weights and the outputs */
+    int32_t rot_dim;     /* leading columns that are rotated: a multiple of 16, 0 .. head_dim */
+    float   eps;         /* of the norm, >= 0 */
+    uint32_t flags;      /* EC_ROPE_* */
+} ec_rope_desc;
+
+/* For every row r and head, x = q[r, h, :] or k[r, h, :]:
+ *     y = x * w / sqrt(mean(x^2) + eps)      with weights w [head_dim]; y = x where both weights are NULL
+ *     y'_a = y_a cos(t) - y_b sin(t), y'_b = y_b cos(t) + y_a sin(t)  for pair i = (a, b) < rot_dim / 2,
+ *     t = positions[r] * inv_freq[i], formed and reduced in 64 bits; everything else in fp32, rounded once.
+ * This makes the post-RoPE q and k_new that ec_attend takes (there n_rows = batch * n_active).
+ * q, k: rows q_row_stride, k_row_stride elements apart (a slice of a packed projection), heads contiguous; q_out, k_out
+ * are dense [n_rows, heads, head_dim] and may be q and k themselves where those are dense.  positions int32 [n_rows]:
+ * a row with a negative one is padding, its outputs are left as they were.  inv_freq fp32 [rot_dim / 2] (may be NULL
+ * when rot_dim is 0).  q_weight and k_weight are both given or both NULL. */
+ec_status ec_qk_norm_rope(const ec_rope_desc *desc, const void *q, int64_t q_row_stride, const void *k,
+                          int64_t k_row_stride, const void *q_weight, const void *k_weight, const int32_t *positions,
+                          const float *inv_freq, int32_t n_rows, void *q_out, void *k_out, void *stream);
+
+/* The same with K going into the pages, next to V (copied verbatim): row r of sequence b to position positions[r] of
+ * that sequence.  Geometry (heads, head_dim, dtype) must agree between the two descriptors; mask_block and scale are
+ * ignored.  Positions must be unique within a sequence.  Rows behind row_offsets[batch] and rows with a negative position
+ * are left alone; a position at or beyond max_pages * page_size sets *dev_status to EC_ERR_SHAPE, a page id outside the
+ * pool to EC_ERR_PAGE, and the row's K and V are not written (its q_out is). */
+ec_status ec_qk_norm_rope_paged(const ec_rope_desc *desc, const ec_paged_desc *paged, const void *q,
+                                int64_t q_row_stride, const void *k, int64_t k_row_stride, const void *v,
+                                int64_t v_row_stride, const void *q_weight, const void *k_weight,
+                                const int32_t *row_offsets, const int32_t *positions, const float *inv_freq,
+                                int32_t n_rows, const int32_t *page_table, void *q_out, void *k_pages, void *v_pages,
+                                int32_t *dev_status, void *stream);
+
+/* ---- Pages: who has which ----------------------------------------------------------------------------------------
+ * State, all DEVICE int32, changed in place: page_table [batch, max_pages], kv_lens [batch], ref_counts [n_pages] (how
+ * many table entries name the page; 0 = free).  The entries in use of sequence b are its first
+ * ceil(kv_lens[b] / page_size); the rest of a row is not read.  Every call is deterministic: pages are handed out lowest
+ * id first, in the order (sequence, entry).  The calls move no K or V: they leave pairs (copy_src[i], copy_dst[i]),
+ * i < *n_copies, for ec_pages_copy; entries behind are -1.  Sources and destinations of one call are disjoint.
+ * batch <= EC_PAGED_MAX_BATCH. */
+typedef struct {
+    int32_t batch, max_pages, n_pages, page_size;   /* page_size: any >= 1 */
+} ec_pages_desc;
+
+/* Bytes of workspace ec_pages_reserve and ec_pages_compact need (0 on bad arguments). */
+size_t ec_pages_workspace_bytes(int32_t n_pages);
+
+/* dst[i] becomes a copy of src[i] that shares all its pages (i < n; n <= batch): table entries and length are taken over,
+ * the pages' counts go up by one each.  The state before the call counts for all pairs.  dst[i] must be empty (length 0);
+ * a pair with an index outside [0, batch), a dst that is not empty or one that an earlier pair names is skipped and
+ * sets *dev_status to EC_ERR_SHAPE.  src may repeat. */
+ec_status ec_pages_fork(const ec_pages_desc *desc, int32_t *page_table, int32_t *kv_lens, int32_t *ref_counts,
+                        const int32_t *src, const int32_t *dst, int32_t n, int32_t *dev_status, void *stream);
+
+/* Before positions write_from[b] .. new_lens[b] - 1 of the sequences are written: afterwards kv_lens[b] =
+ * max(kv_lens[b], new_lens[b]) and every page that holds one of these positions belongs to sequence b alone.  Missing pages
+ * are taken from the free ones; a page in use that was shared when the call began is replaced by a free one and leaves
+ * a pair to copy.  (Where all owners of a page write, each gets a copy and the page becomes free.)
+ * All or nothing: with too few free pages, a new length beyond max_pages * page_size or more than copy_cap pairs, the
+ * state stays as it was, *n_copies is 0 and *dev_status EC_ERR_PAGE. copy_src, copy_dst: [copy_cap]. */
+ec_status ec_pages_reserve(const ec_pages_desc *desc, int32_t *page_table, int32_t *kv_lens, int32_t *ref_counts,
+                           const int32_t *write_from, const int32_t *new_lens, int32_t *copy_src, int32_t *copy_dst,
+                           int32_t copy_cap, int32_t *n_copies, void *workspace, size_t workspace_bytes,
+                           int32_t *dev_status, void *stream);
+
+/* Every sequence is cut to keep_lens[b] positions (0 frees it; values >= kv_lens[b] leave it alone, negative ones count
+ * as 0): the counts of the pages behind go down by one each and their entries become -1. */
+ec_status ec_pages_release(const ec_pages_desc *desc, int32_t *page_table, int32_t *kv_lens, int32_t *ref_counts,
+                           const int32_t *keep_lens, void *stream);
+
+/* Moves the pages in use together: with u pages in use, the ones with ids >= u, ascending, take the free ids < u,
+ * ascending; table entries and counts follow.  copy_src, copy_dst: [copy_cap], copy_cap >= n_pages / 2. */
+ec_status ec_pages_compact(const ec_pages_desc *desc, int32_t *page_table, int32_t *kv_lens, int32_t *ref_counts,
+                           int32_t *copy_src, int32_t *copy_dst, int32_t copy_cap, int32_t *n_copies, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
+/* Page copy_src[i] -> copy_dst[i] for i < min(*n_copies, copy_cap), in K and V of n_layers pools that stand layer_bytes
+ * apart (n_copies NULL: copy_cap pairs).  page_bytes and layer_bytes are multiples of 16.  Pairs with an id
+ * outside [0, n_pages) are skipped and set *dev_status to EC_ERR_PAGE.  No page may be both a source and a destination. */
+ec_status ec_pages_copy(void *k_pages, void *v_pages, int64_t page_bytes, int32_t n_pages, int32_t n_layers,
+                        int64_t layer_bytes, const int32_t *copy_src, const int32_t *copy_dst, int32_t copy_cap,
+                        const int32_t *n_copies, int32_t *dev_status, void *stream);
+
+/* ---- Sampling ---------------------------------------------------------------------------------------------------- */
+
+/* Bytes of workspace ec_sample needs (0 on bad arguments). */
+size_t ec_sample_workspace_bytes(int32_t n_rows, int32_t vocab);
+
+/* One token per logits row from a given uniform number (the gate decodes the argmax; this is the sampled form).  Per
+ * row, with z_j = logits_j / temperature and w_j = exp(z_j - max z), tokens ordered by logit, descending, the lower index
+ * first on ties, tokens of logit -inf left out:
+ *     n_k = min(top_k, tokens)            (top_k <= 0: all)
+ *     n_p = the fewest leading tokens whose w sum to at least top_p * (the sum over the first n_k)   (top_p >= 1: n_k;
+ *           at least one token)
+ *     n_m = the tokens with w_j >= min_p, at least one                                  (min_p <= 0: all)
+ *     kept_out  = n = min(n_k, n_p, n_m)
+ *     token_out = the first of the n whose running sum of w exceeds u * S, S = their sum; the n-th if none does
+ *     prob_out  = w[token] / S
+ * temperature <= 0 decodes greedily (token = argmax, prob = 1, kept = 1).  A row without a finite token gives token -1, prob
+ * 0, kept 0.  logits: [n_rows, row_stride_elems] of `dtype`, the first `vocab` columns are read; +inf and NaN are
+ * not allowed (that row's outputs are unspecified).  temperature, top_p, min_p fp32 [n_rows], top_k int32 [n_rows]:
+ * each may be NULL (1, off, off, off).  u fp32 [n_rows], in [0, 1).  Weights are formed in 64 bits and summed as
+ * integers in units of 2^-43 of the largest or finer (2^-47 up to 32768 columns, 2^-45 at 126464), so results do not
+ * depend on how the work is split.  prob_out and kept_out may
+ * be NULL.  vocab <= 1048576.  All DEVICE pointers; rows 16-byte aligned as for ec_entropy_gate. */
+ec_status ec_sample(const void *logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t row_stride_elems,
+                    const float *u, const float *temperature, const int32_t *top_k, const float *top_p,
+                    const float *min_p, int32_t *token_out, float *prob_out, int32_t *kept_out, void *workspace,
+                    size_t workspace_bytes, void *stream);
 
 /* Zero-fills a workspace (asynchronous on `stream`). */
 ec_status ec_workspace_init(void *workspace, size_t workspace_bytes, void *stream);

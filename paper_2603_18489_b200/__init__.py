@@ -28,6 +28,8 @@ LIB_PATH = os.path.join(_HERE, "libentropycache.so")
 EC_F32, EC_BF16 = 0, 1
 EC_SKIP, EC_RECOMPUTE = 0, 1
 EC_ATTN_CACHE_SETTLED = 1   # ec_attn_desc.flags: nothing in flight on the stream writes the caches
+EC_ROPE_INTERLEAVED = 1     # ec_rope_desc.flags: the rotated pairs are columns (2i, 2i+1)
+EC_PAGED_MAX_BATCH = 1024
 EC_OK = 0
 
 
@@ -42,6 +44,20 @@ class ec_attn_desc(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("ctx_len", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
                 ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class ec_paged_desc(ctypes.Structure):
+    """Mirror of the C struct ec_paged_desc."""
+    _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("mask_block", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class ec_rope_desc(ctypes.Structure):
+    """Mirror of the C struct ec_rope_desc."""
+    _fields_ = [("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("eps", ctypes.c_float), ("flags", ctypes.c_uint32)]
 
 
 def _load() -> ctypes.CDLL:
@@ -76,6 +92,15 @@ def _load() -> ctypes.CDLL:
     lib.ec_select_recent.restype = i32
     lib.ec_select_recent_sliding.argtypes = [vp, i32, i32, vp, vp, vp, i32, vp, i32, vp, i32, vp]
     lib.ec_select_recent_sliding.restype = i32
+    pd = ctypes.POINTER(ec_paged_desc)
+    lib.ec_attend_paged_workspace_bytes.argtypes = [pd, i32]
+    lib.ec_attend_paged_workspace_bytes.restype = sz
+    lib.ec_attend_paged_kernel_name.argtypes = [pd, i32]
+    lib.ec_attend_paged_kernel_name.restype = ctypes.c_char_p
+    lib.ec_pages_workspace_bytes.argtypes = [i32]
+    lib.ec_pages_workspace_bytes.restype = sz
+    lib.ec_sample_workspace_bytes.argtypes = [i32, i32]
+    lib.ec_sample_workspace_bytes.restype = sz
     lib.ec_workspace_init.argtypes = [vp, sz, vp]
     lib.ec_workspace_init.restype = i32
     lib.ec_status_string.argtypes = [i32]
@@ -287,3 +312,161 @@ def ec_select_recent_sliding(history, state, masked, decoded_flags, window: int,
     status = _native.select_recent_sliding(history, state, masked, decoded_flags, window, decision, k, active_idx, stream)
     if status:
         raise EcError(status, "ec_select_recent_sliding")
+
+
+# ---- paged cache, rotation, sampling ---------------------------------------------------------------------------------
+def _type_code(dtype) -> int:
+    if isinstance(dtype, int):
+        return dtype
+    if dtype == torch.bfloat16:
+        return EC_BF16
+    if dtype == torch.float32:
+        return EC_F32
+    raise TypeError(f"unsupported element type {dtype}")
+
+
+def make_paged_desc(batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype, page_size: int, n_pages: int,
+                    max_pages: int, mask_block: int = 0, scale: float = 0.0) -> ec_paged_desc:
+    """mask_block: 0 every row sees all keys (bidirectional), 1 causal, m > 1 rows of a block of m positions see the
+    whole block and what stands before it."""
+    return ec_paged_desc(batch, n_q_heads, n_kv_heads, head_dim, _type_code(dtype), page_size, n_pages, max_pages, mask_block,
+                         scale, 0)
+
+
+def make_rope_desc(n_q_heads: int, n_kv_heads: int, head_dim: int, dtype, rot_dim: int, eps: float = 1e-6,
+                   interleaved: bool = False) -> ec_rope_desc:
+    return ec_rope_desc(n_q_heads, n_kv_heads, head_dim, _type_code(dtype), rot_dim, eps,
+                        EC_ROPE_INTERLEAVED if interleaved else 0)
+
+
+def ec_attend_paged_workspace_bytes(desc: ec_paged_desc, max_rows: int) -> int:
+    return int(lib.ec_attend_paged_workspace_bytes(ctypes.byref(desc), int(max_rows)))
+
+
+def ec_attend_paged_kernel_name(desc: ec_paged_desc, max_rows: int) -> str:
+    """Host-only: which kernel ec_attend_paged picks."""
+    return lib.ec_attend_paged_kernel_name(ctypes.byref(desc), int(max_rows)).decode()
+
+
+def ec_pages_workspace_bytes(n_pages: int) -> int:
+    return int(lib.ec_pages_workspace_bytes(int(n_pages)))
+
+
+def ec_sample_workspace_bytes(n_rows: int, vocab: int) -> int:
+    return int(lib.ec_sample_workspace_bytes(int(n_rows), int(vocab)))
+
+
+def ec_attend_paged(desc: ec_paged_desc, q, row_offsets, kv_lens, max_rows: int, page_table, k_pages, v_pages, out=None,
+                    workspace=None, dev_status=None, stream=None) -> torch.Tensor:
+    """Attention of a ragged chunk of new rows over a paged cache.  q [n_rows, H_q, D]; row_offsets int32 [B + 1], kv_lens
+    int32 [B], page_table int32 [B, max_pages] (read on the device); k_pages, v_pages [n_pages, H_kv, page_size, D].
+    Returns `out` [n_rows, H_q, D]; rows behind row_offsets[B] are left as they were."""
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if workspace is None:
+        with torch.cuda.device(q.device):
+            workspace = new_workspace(ec_attend_paged_workspace_bytes(desc, max_rows), q.device)
+    status = _native.attend_paged(desc, q, row_offsets, kv_lens, max_rows, page_table, k_pages, v_pages, out, workspace,
+                                  dev_status, stream)
+    if status:
+        raise EcError(status, "ec_attend_paged")
+    return out
+
+
+def ec_qk_norm_rope(desc: ec_rope_desc, q, k, positions, inv_freq, q_weight=None, k_weight=None, q_out=None, k_out=None,
+                    stream=None):
+    """Norms of the query and key heads (if weights are given) and the position rotation in one pass.  q [..., H_q, D], k
+    [..., H_kv, D]: rows may be slices of a packed projection; positions int32, one a row; inv_freq fp32 [rot_dim / 2].
+    Returns (q_out, k_out), dense."""
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    status = _native.qk_norm_rope(desc, q, k, q_weight, k_weight, positions, inv_freq, q_out, k_out, stream)
+    if status:
+        raise EcError(status, "ec_qk_norm_rope")
+    return q_out, k_out
+
+
+def ec_qk_norm_rope_paged(desc: ec_rope_desc, paged: ec_paged_desc, q, k, v, row_offsets, positions, inv_freq, page_table,
+                          k_pages, v_pages, q_weight=None, k_weight=None, q_out=None, dev_status=None,
+                          stream=None) -> torch.Tensor:
+    """ec_qk_norm_rope with K, and V as it is, going into the pages at the rows' positions.  Returns q_out, dense."""
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    status = _native.qk_norm_rope_paged(desc, paged, q, k, v, q_weight, k_weight, row_offsets, positions, inv_freq, page_table,
+                                        q_out, k_pages, v_pages, dev_status, stream)
+    if status:
+        raise EcError(status, "ec_qk_norm_rope_paged")
+    return q_out
+
+
+def ec_sample(logits, vocab: int, u, temperature=None, top_k=None, top_p=None, min_p=None, *, token_out=None, prob_out=None,
+              kept_out=None, workspace=None, stream=None) -> dict:
+    """One token per logits row [R, row_stride] from the uniform numbers u fp32 [R]; temperature, top_p, min_p fp32 [R]
+    and top_k int32 [R], each may be None.  Outputs are device tensors; nothing is synchronised."""
+    rows, device = logits.shape[0], logits.device
+    if token_out is None:
+        token_out = torch.empty(rows, dtype=torch.int32, device=device)
+    if prob_out is None:
+        prob_out = torch.empty(rows, dtype=torch.float32, device=device)
+    if kept_out is None:
+        kept_out = torch.empty(rows, dtype=torch.int32, device=device)
+    if workspace is None:
+        workspace = new_workspace(ec_sample_workspace_bytes(rows, vocab), device)
+    status = _native.sample(logits, vocab, u, temperature, top_k, top_p, min_p, token_out, prob_out, kept_out, workspace, stream)
+    if status:
+        raise EcError(status, "ec_sample")
+    return dict(token=token_out, prob=prob_out, kept=kept_out)
+
+
+def new_pages(batch: int, max_pages: int, n_pages: int, device="cuda"):
+    """(page_table, kv_lens, ref_counts) of a pool that nobody uses."""
+    return (torch.full((batch, max_pages), -1, dtype=torch.int32, device=device),
+            torch.zeros(batch, dtype=torch.int32, device=device), torch.zeros(n_pages, dtype=torch.int32, device=device))
+
+
+def ec_pages_fork(page_table, kv_lens, ref_counts, src, dst, page_size: int, dev_status=None, stream=None) -> None:
+    """Sequence dst[i] (empty) becomes a copy of src[i] that shares its pages."""
+    status = _native.pages_fork(page_table, kv_lens, ref_counts, page_size, src, dst, dev_status, stream)
+    if status:
+        raise EcError(status, "ec_pages_fork")
+
+
+def ec_pages_reserve(page_table, kv_lens, ref_counts, write_from, new_lens, page_size: int, copy_src, copy_dst, n_copies, *,
+                     workspace=None, dev_status=None, stream=None) -> None:
+    """Before positions write_from[b] .. new_lens[b] - 1 are written: missing pages are taken, shared ones replaced.  The
+    pairs (copy_src[i], copy_dst[i]), i < n_copies, are for ec_pages_copy."""
+    if workspace is None:
+        workspace = new_workspace(ec_pages_workspace_bytes(ref_counts.numel()), page_table.device)
+    status = _native.pages_reserve(page_table, kv_lens, ref_counts, page_size, write_from, new_lens, copy_src, copy_dst, n_copies,
+                                   workspace, dev_status, stream)
+    if status:
+        raise EcError(status, "ec_pages_reserve")
+
+
+def ec_pages_release(page_table, kv_lens, ref_counts, keep_lens, page_size: int, stream=None) -> None:
+    """Every sequence is cut to keep_lens[b] positions; 0 frees it."""
+    status = _native.pages_release(page_table, kv_lens, ref_counts, page_size, keep_lens, stream)
+    if status:
+        raise EcError(status, "ec_pages_release")
+
+
+def ec_pages_compact(page_table, kv_lens, ref_counts, page_size: int, copy_src, copy_dst, n_copies, *, workspace=None,
+                     stream=None) -> None:
+    """Moves the pages in use to the lowest ids; the pairs to copy go to copy_src, copy_dst (n_pages / 2 long at least)."""
+    if workspace is None:
+        workspace = new_workspace(ec_pages_workspace_bytes(ref_counts.numel()), page_table.device)
+    status = _native.pages_compact(page_table, kv_lens, ref_counts, page_size, copy_src, copy_dst, n_copies, workspace, stream)
+    if status:
+        raise EcError(status, "ec_pages_compact")
+
+
+def ec_pages_copy(k_pages, v_pages, copy_src, copy_dst, n_copies=None, dev_status=None, stream=None) -> None:
+    """Page copy_src[i] -> copy_dst[i] in K and V.  Pools [n_pages, H_kv, page_size, D], or all layers' in one tensor
+    [n_layers, n_pages, H_kv, page_size, D].  n_copies int32 [1] (None: every pair of the lists)."""
+    if k_pages.dim() not in (4, 5):
+        raise ValueError("k_pages must be [n_pages, H_kv, page_size, D] or [n_layers, n_pages, H_kv, page_size, D]")
+    status = _native.pages_copy(k_pages, v_pages, copy_src, copy_dst, n_copies, k_pages.dim() == 5, dev_status, stream)
+    if status:
+        raise EcError(status, "ec_pages_copy")

@@ -63,6 +63,10 @@ size_t attend_ws(const ec_attn_desc& d, int n_active) {
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+template <typename... P>
+bool all_aligned4(P... p) { return (aligned4(p) && ...); }
+
 // which kernel serves a call of ec_attend: the one place the dispatch order is written down
 enum AttendPath { PATH_SKIP_KEYS, PATH_SKIP_ROWS, PATH_DENSE_FROM_NEW, PATH_DENSE, PATH_TC_ONE_TILE, PATH_MMA, PATH_F32 };
 AttendPath choose_path(const ec_attn_desc& d, int n_active, bool fresh_kv, bool index_list) {
@@ -334,6 +338,260 @@ ec_status ec_entropy_gate_decode(const void* logits, int32_t dtype, int32_t n_ro
                      nullptr, nullptr, workspace, workspace_bytes, stream);
 }
 
+namespace {
+
+ec_status check_paged(const ec_paged_desc* d) {
+    if (!d) return EC_ERR_NULL;
+    if (d->dtype != EC_F32 && d->dtype != EC_BF16) return EC_ERR_DTYPE;
+    if (d->batch < 1 || d->n_q_heads < 1 || d->n_kv_heads < 1 || d->n_pages < 1 || d->max_pages < 1 || d->mask_block < 0)
+        return EC_ERR_SHAPE;
+    if (d->n_q_heads % d->n_kv_heads != 0) return EC_ERR_SHAPE;
+    if (d->head_dim != 64 && d->head_dim != 128) return EC_ERR_UNSUPPORTED;
+    if (d->page_size != 16 && d->page_size != 32 && d->page_size != 64 && d->page_size != 128) return EC_ERR_UNSUPPORTED;
+    if (d->batch > EC_PAGED_MAX_BATCH || d->n_q_heads / d->n_kv_heads > 128 || d->n_q_heads > 4096) return EC_ERR_UNSUPPORTED;
+    if (!(d->scale >= 0.f) || d->scale > 1.0e30f) return EC_ERR_SHAPE;   // also rejects NaN
+    if (d->flags) return EC_ERR_UNSUPPORTED;
+    return EC_OK;
+}
+ec_status check_rope(const ec_rope_desc* d) {
+    if (!d) return EC_ERR_NULL;
+    if (d->dtype != EC_F32 && d->dtype != EC_BF16) return EC_ERR_DTYPE;
+    if (d->n_q_heads < 1 || d->n_kv_heads < 1) return EC_ERR_SHAPE;
+    if (d->head_dim != 64 && d->head_dim != 128) return EC_ERR_UNSUPPORTED;
+    if (d->rot_dim < 0 || d->rot_dim > d->head_dim || d->rot_dim % 16 != 0) return EC_ERR_SHAPE;
+    if (!(d->eps >= 0.f) || d->eps > 1.0e30f) return EC_ERR_SHAPE;
+    if (d->flags & ~(uint32_t)EC_ROPE_INTERLEAVED) return EC_ERR_UNSUPPORTED;
+    if (d->n_q_heads > 4096 || d->n_kv_heads > 4096) return EC_ERR_UNSUPPORTED;
+    return EC_OK;
+}
+// a tensor of rows `stride` elements apart that holds `heads` heads a row
+ec_status check_rows(const ec_rope_desc& d, const void* p, int64_t stride, int heads) {
+    if (!p) return EC_ERR_NULL;
+    if (stride < (int64_t)heads * d.head_dim) return EC_ERR_SHAPE;
+    const int64_t e = d.dtype == EC_BF16 ? 2 : 4;
+    return aligned16(p) && stride * e % 16 == 0 ? EC_OK : EC_ERR_ALIGN;
+}
+ec_status rope_call(const ec_rope_desc* desc, const void* q, int64_t q_row_stride, const void* k, int64_t k_row_stride,
+                    const void* q_weight, const void* k_weight, const int32_t* positions, const float* inv_freq,
+                    int32_t n_rows, void* q_out, void* k_out, RopeArgs& a, void* stream) {
+    if ((q_weight == nullptr) != (k_weight == nullptr) || !positions || !q_out || !k_out || (desc->rot_dim > 0 && !inv_freq))
+        return EC_ERR_NULL;
+    ec_status st = check_rows(*desc, q, q_row_stride, desc->n_q_heads);
+    if (st == EC_OK) st = check_rows(*desc, k, k_row_stride, desc->n_kv_heads);
+    if (st != EC_OK) return st;
+    if (!aligned16(q_out) || !aligned16(k_out) || !aligned16(q_weight) || !aligned16(k_weight) || !all_aligned4(positions, inv_freq))
+        return EC_ERR_ALIGN;
+    a.d = *desc;
+    a.q = q, a.k = k;
+    a.q_stride = q_row_stride, a.k_stride = k_row_stride;
+    a.q_weight = q_weight, a.k_weight = k_weight;
+    a.positions = positions;
+    a.inv_freq = inv_freq;
+    a.n_rows = n_rows;
+    a.q_out = q_out, a.k_out = k_out;
+    return launch_rope(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? EC_OK : EC_ERR_CUDA;
+}
+
+size_t paged_ws(const ec_paged_desc& d) { return attend_paged_rows_workspace(d); }
+
+ec_status check_pages(const ec_pages_desc* d, const int32_t* table, const int32_t* lens, const int32_t* refs) {
+    if (!d || !table || !lens || !refs) return EC_ERR_NULL;
+    if (d->batch < 1 || d->max_pages < 1 || d->n_pages < 1 || d->page_size < 1) return EC_ERR_SHAPE;
+    if (d->batch > EC_PAGED_MAX_BATCH || d->n_pages > (1 << 28) || (long long)d->max_pages * d->page_size > 0x7fffff00ll)
+        return EC_ERR_UNSUPPORTED;
+    return all_aligned4(table, lens, refs) ? EC_OK : EC_ERR_ALIGN;
+}
+
+}  // namespace
+
+ec_status ec_qk_norm_rope(const ec_rope_desc* desc, const void* q, int64_t q_row_stride, const void* k, int64_t k_row_stride,
+                          const void* q_weight, const void* k_weight, const int32_t* positions, const float* inv_freq,
+                          int32_t n_rows, void* q_out, void* k_out, void* stream) {
+    const ec_status st = check_rope(desc);
+    if (st != EC_OK) return st;
+    if (n_rows < 0) return EC_ERR_SHAPE;
+    if (n_rows == 0) return EC_OK;
+    RopeArgs a;
+    a.v = nullptr;
+    a.v_stride = 0;
+    return rope_call(desc, q, q_row_stride, k, k_row_stride, q_weight, k_weight, positions, inv_freq, n_rows, q_out, k_out, a, stream);
+}
+
+ec_status ec_qk_norm_rope_paged(const ec_rope_desc* desc, const ec_paged_desc* paged, const void* q, int64_t q_row_stride,
+                                const void* k, int64_t k_row_stride, const void* v, int64_t v_row_stride,
+                                const void* q_weight, const void* k_weight, const int32_t* row_offsets,
+                                const int32_t* positions, const float* inv_freq, int32_t n_rows, const int32_t* page_table,
+                                void* q_out, void* k_pages, void* v_pages, int32_t* dev_status, void* stream) {
+    ec_status st = check_rope(desc);
+    if (st == EC_OK) st = check_paged(paged);
+    if (st != EC_OK) return st;
+    if (desc->n_q_heads != paged->n_q_heads || desc->n_kv_heads != paged->n_kv_heads || desc->head_dim != paged->head_dim ||
+        n_rows < 0)
+        return EC_ERR_SHAPE;
+    if (desc->dtype != paged->dtype) return EC_ERR_DTYPE;
+    if (n_rows == 0) return EC_OK;
+    if (!row_offsets || !page_table || !v_pages) return EC_ERR_NULL;
+    st = check_rows(*desc, v, v_row_stride, desc->n_kv_heads);
+    if (st != EC_OK) return st;
+    if (!aligned16(v_pages) || !all_aligned4(row_offsets, page_table, dev_status)) return EC_ERR_ALIGN;
+    RopeArgs a;
+    a.v = v;
+    a.v_stride = v_row_stride;
+    a.v_pages = v_pages;
+    a.row_offsets = row_offsets;
+    a.page_table = page_table;
+    a.batch = paged->batch;
+    a.page_size = paged->page_size;
+    a.n_pages = paged->n_pages;
+    a.max_pages = paged->max_pages;
+    a.dev_status = dev_status;
+    return rope_call(desc, q, q_row_stride, k, k_row_stride, q_weight, k_weight, positions, inv_freq, n_rows, q_out, k_pages, a, stream);
+}
+
+size_t ec_attend_paged_workspace_bytes(const ec_paged_desc* desc, int32_t max_rows) {
+    if (check_paged(desc) != EC_OK || max_rows < 1) return 0;
+    return paged_ws(*desc);
+}
+
+ec_status ec_attend_paged(const ec_paged_desc* desc, const void* q, const int32_t* row_offsets, const int32_t* kv_lens,
+                          int32_t n_rows, int32_t max_rows, const int32_t* page_table, const void* k_pages,
+                          const void* v_pages, void* out, void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                          void* stream) {
+    const ec_status st = check_paged(desc);
+    if (st != EC_OK) return st;
+    if (n_rows < 0 || max_rows < 1) return EC_ERR_SHAPE;
+    if (n_rows == 0) return EC_OK;
+    if (!q || !row_offsets || !kv_lens || !page_table || !k_pages || !v_pages || !out) return EC_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) ||
+        !all_aligned4(row_offsets, kv_lens, page_table, dev_status))
+        return EC_ERR_ALIGN;
+    if (!workspace || workspace_bytes < paged_ws(*desc)) return EC_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return EC_ERR_ALIGN;
+    PagedArgs a;
+    a.d = *desc;
+    a.q = q;
+    a.row_offsets = row_offsets;
+    a.kv_lens = kv_lens;
+    a.n_rows = n_rows;
+    a.max_rows = max_rows;
+    a.page_table = page_table;
+    a.k_pages = k_pages;
+    a.v_pages = v_pages;
+    a.out = out;
+    a.workspace = workspace;
+    a.dev_status = dev_status;
+    a.scale = desc->scale > 0.f ? desc->scale : 1.0f / sqrtf((float)desc->head_dim);
+    return launch_attend_paged_rows(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? EC_OK : EC_ERR_CUDA;
+}
+
+const char* ec_attend_paged_kernel_name(const ec_paged_desc* desc, int32_t max_rows) {
+    if (check_paged(desc) != EC_OK || max_rows < 1) return "";
+    return "attend_paged_rows_kernel";
+}
+
+size_t ec_pages_workspace_bytes(int32_t n_pages) { return n_pages < 1 || n_pages > (1 << 28) ? 0 : pages_workspace_bytes(n_pages); }
+
+ec_status ec_pages_fork(const ec_pages_desc* desc, int32_t* page_table, int32_t* kv_lens, int32_t* ref_counts,
+                        const int32_t* src, const int32_t* dst, int32_t n, int32_t* dev_status, void* stream) {
+    const ec_status st = check_pages(desc, page_table, kv_lens, ref_counts);
+    if (st != EC_OK) return st;
+    if (n < 0 || n > desc->batch) return EC_ERR_SHAPE;
+    if (n == 0) return EC_OK;
+    if (!src || !dst) return EC_ERR_NULL;
+    if (!all_aligned4(src, dst, dev_status)) return EC_ERR_ALIGN;
+    return launch_pages_fork(*desc, page_table, kv_lens, ref_counts, src, dst, n, dev_status, static_cast<cudaStream_t>(stream)) ==
+                   cudaSuccess ? EC_OK : EC_ERR_CUDA;
+}
+
+ec_status ec_pages_reserve(const ec_pages_desc* desc, int32_t* page_table, int32_t* kv_lens, int32_t* ref_counts,
+                           const int32_t* write_from, const int32_t* new_lens, int32_t* copy_src, int32_t* copy_dst,
+                           int32_t copy_cap, int32_t* n_copies, void* workspace, size_t workspace_bytes,
+                           int32_t* dev_status, void* stream) {
+    const ec_status st = check_pages(desc, page_table, kv_lens, ref_counts);
+    if (st != EC_OK) return st;
+    if (copy_cap < 0) return EC_ERR_SHAPE;
+    if (!write_from || !new_lens || !n_copies || (copy_cap > 0 && (!copy_src || !copy_dst))) return EC_ERR_NULL;
+    if (!all_aligned4(write_from, new_lens, copy_src, copy_dst, n_copies, dev_status)) return EC_ERR_ALIGN;
+    if (!workspace || workspace_bytes < pages_workspace_bytes(desc->n_pages)) return EC_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return EC_ERR_ALIGN;
+    return launch_pages_reserve(*desc, page_table, kv_lens, ref_counts, write_from, new_lens, copy_src, copy_dst, copy_cap,
+                                n_copies, workspace, dev_status, static_cast<cudaStream_t>(stream)) == cudaSuccess ? EC_OK : EC_ERR_CUDA;
+}
+
+ec_status ec_pages_release(const ec_pages_desc* desc, int32_t* page_table, int32_t* kv_lens, int32_t* ref_counts,
+                           const int32_t* keep_lens, void* stream) {
+    const ec_status st = check_pages(desc, page_table, kv_lens, ref_counts);
+    if (st != EC_OK) return st;
+    if (!keep_lens) return EC_ERR_NULL;
+    if (!aligned4(keep_lens)) return EC_ERR_ALIGN;
+    return launch_pages_release(*desc, page_table, kv_lens, ref_counts, keep_lens, static_cast<cudaStream_t>(stream)) == cudaSuccess
+               ? EC_OK : EC_ERR_CUDA;
+}
+
+ec_status ec_pages_compact(const ec_pages_desc* desc, int32_t* page_table, int32_t* kv_lens, int32_t* ref_counts,
+                           int32_t* copy_src, int32_t* copy_dst, int32_t copy_cap, int32_t* n_copies, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+    const ec_status st = check_pages(desc, page_table, kv_lens, ref_counts);
+    if (st != EC_OK) return st;
+    if (copy_cap < desc->n_pages / 2) return EC_ERR_SHAPE;
+    if (!n_copies || (copy_cap > 0 && (!copy_src || !copy_dst))) return EC_ERR_NULL;
+    if (!all_aligned4(copy_src, copy_dst, n_copies)) return EC_ERR_ALIGN;
+    if (!workspace || workspace_bytes < pages_workspace_bytes(desc->n_pages)) return EC_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return EC_ERR_ALIGN;
+    return launch_pages_compact(*desc, page_table, kv_lens, ref_counts, copy_src, copy_dst, copy_cap, n_copies, workspace,
+                                static_cast<cudaStream_t>(stream)) == cudaSuccess ? EC_OK : EC_ERR_CUDA;
+}
+
+ec_status ec_pages_copy(void* k_pages, void* v_pages, int64_t page_bytes, int32_t n_pages, int32_t n_layers,
+                        int64_t layer_bytes, const int32_t* copy_src, const int32_t* copy_dst, int32_t copy_cap,
+                        const int32_t* n_copies, int32_t* dev_status, void* stream) {
+    if (page_bytes < 1 || n_pages < 1 || n_layers < 1 || copy_cap < 0) return EC_ERR_SHAPE;
+    if (n_layers > 1 && layer_bytes / n_pages < page_bytes) return EC_ERR_SHAPE;
+    if (copy_cap == 0) return EC_OK;
+    if (!k_pages || !v_pages || !copy_src || !copy_dst) return EC_ERR_NULL;
+    if (!aligned16(k_pages) || !aligned16(v_pages) || page_bytes % 16 || layer_bytes % 16 ||
+        !all_aligned4(copy_src, copy_dst, n_copies, dev_status))
+        return EC_ERR_ALIGN;
+    if (page_bytes > (1ll << 31)) return EC_ERR_UNSUPPORTED;
+    return launch_pages_copy(k_pages, v_pages, page_bytes, n_pages, n_layers, layer_bytes, copy_src, copy_dst, copy_cap, n_copies,
+                             dev_status, static_cast<cudaStream_t>(stream)) == cudaSuccess ? EC_OK : EC_ERR_CUDA;
+}
+
+size_t ec_sample_workspace_bytes(int32_t n_rows, int32_t vocab) {
+    return n_rows < 0 || vocab < 1 || vocab > (1 << 20) ? 0 : sample_workspace_bytes(n_rows, vocab);
+}
+
+ec_status ec_sample(const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t row_stride_elems, const float* u,
+                    const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                    int32_t* token_out, float* prob_out, int32_t* kept_out, void* workspace, size_t workspace_bytes,
+                    void* stream) {
+    if (dtype != EC_F32 && dtype != EC_BF16) return EC_ERR_DTYPE;
+    if (n_rows < 0 || vocab < 1 || row_stride_elems < vocab) return EC_ERR_SHAPE;
+    if (vocab > (1 << 20) || n_rows > (1 << 24)) return EC_ERR_UNSUPPORTED;
+    if (n_rows == 0) return EC_OK;
+    if (!logits || !u || !token_out) return EC_ERR_NULL;
+    if (!aligned16(logits) || row_stride_elems * (dtype == EC_BF16 ? 2 : 4) % 16 != 0 ||
+        !all_aligned4(u, temperature, top_k, top_p, min_p, token_out, prob_out, kept_out))
+        return EC_ERR_ALIGN;
+    if (!workspace || workspace_bytes < sample_workspace_bytes(n_rows, vocab)) return EC_ERR_WORKSPACE;
+    SampleArgs a;
+    a.logits = logits;
+    a.dtype = dtype;
+    a.n_rows = n_rows;
+    a.vocab = vocab;
+    a.row_stride = row_stride_elems;
+    a.u = u;
+    a.temperature = temperature;
+    a.top_k = top_k;
+    a.top_p = top_p;
+    a.min_p = min_p;
+    a.token_out = token_out;
+    a.prob_out = prob_out;
+    a.kept_out = kept_out;
+    a.workspace = workspace;
+    return launch_sample(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? EC_OK : EC_ERR_CUDA;
+}
+
 ec_status ec_workspace_init(void* workspace, size_t workspace_bytes, void* stream) {
     if (workspace_bytes == 0) return EC_OK;
     if (!workspace) return EC_ERR_NULL;
@@ -353,6 +611,7 @@ const char* ec_status_string(int32_t status) {
         case EC_ERR_UNSUPPORTED: return "EC_ERR_UNSUPPORTED: outside what the kernels implement";
         case EC_ERR_CUDA: return "EC_ERR_CUDA: a CUDA runtime call or launch failed";
         case EC_ERR_TIMEOUT: return "EC_ERR_TIMEOUT: a bounded device-side wait gave up";
+        case EC_ERR_PAGE: return "EC_ERR_PAGE: a page id outside the pool, or no free pages left";
         default: return "unknown ec_status";
     }
 }

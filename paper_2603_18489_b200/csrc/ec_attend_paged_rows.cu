@@ -1,0 +1,438 @@
+// ec_attend_paged for few query rows a kv head (decoding: one row a sequence) in bf16, and for fp32: sixteen packed query
+// rows a tile, the keys split over warps that know nothing of one another until the end.
+//
+// Bound by the K/V bytes.  A CTA's four warps take the key tiles of 64 keys, a warp sixteen of them: it loads its own
+// chunk of K and V (rows of one page; cp.async, three stages deep, zeros behind the sequence's end, so that
+// what an unfinished page holds is never multiplied), forms the scores, keeps its own running maximum and sum, and multiplies
+// into its own accumulators.  Nothing but the merge of the four at the end of a unit's keys needs the CTA together.
+//   bf16   mma.sync m16n8k16 (the sixteen rows are its M; tcgen05 has no shape below 64 rows, and this is far from
+//          bound by the tensor pipe), P rounded to bf16 for the second product as the dense kernels do
+//   fp32   FMA units; a lane has one key and eight rows for the scores, HD / 32 columns of all rows for the output
+// The work is cut as ec_paged.cuh says; combine_kernel joins the units that a cut divided.
+#include "ec_paged.cuh"
+#include "ec_paged_combine.cuh"
+#include "ec_tc_ptx.cuh"
+
+namespace ec {
+namespace {
+
+using namespace paged;
+
+constexpr int kWarps = 4, kThreads = 32 * kWarps, kStages = 3;
+constexpr int TM = 16, CK = 16, TK = CK * kWarps;
+
+template <typename T, int HD>
+struct Geo {
+    static constexpr int CHUNK = CK * HD * (int)sizeof(T);   // bytes of a warp's K or V chunk
+    static constexpr int STAGE = 2 * CHUNK;
+    static constexpr int WARP = kStages * STAGE;
+    static constexpr int Q = sizeof(T) == 4 ? TM * HD * 4 : 0;        // fp32: the tile's query rows ...
+    static constexpr int P = sizeof(T) == 4 ? kWarps * CK * TM * 4 : 0;   // ... and the probabilities
+    static constexpr int BYTES = kWarps * WARP + Q + P;
+    static constexpr int CTAS = (BYTES + 10240) * 3 <= 228 * 1024 ? 3 : (BYTES + 10240) * 2 <= 228 * 1024 ? 2 : 1;   // an SM
+};
+
+struct Params {
+    Plan plan;
+    const void *q, *k, *v;
+    void* out;
+    float* partial;
+    long long* cuts;
+    const int32_t* page_table;
+    int page_shift, n_pages, max_pages, n_q_heads;
+    float scale_log2;
+};
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool valid) {
+    const uint32_t bytes = valid ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void ldsm(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm_t(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// A warp's state over its chunks.  Row limits: a key counts for a row while it is below lim.
+template <int HD>
+struct WarpBf16 {
+    uint32_t qa[HD / 16][4];
+    float o[HD / 8][4], m[2], l[2];
+    int lim[2];
+    __device__ __forceinline__ void start(const Params& p, const Unit& u, int lane, const unsigned char*) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int pr = u.tile * TM + lane / 4 + 8 * h, tok = pr / p.plan.group;
+            const bool has = tok < u.s.n;
+            lim[h] = has ? limit_of(p.plan, u.s, tok) : 0;
+            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q) +
+                ((long long)(u.s.row0 + tok) * p.n_q_heads + u.head * p.plan.group + pr % p.plan.group) * HD + (lane & 3) * 2;
+#pragma unroll
+            for (int ks = 0; ks < HD / 16; ++ks) {
+                qa[ks][h] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16) : 0u;
+                qa[ks][2 + h] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + 8) : 0u;
+            }
+            m[h] = -INFINITY;
+            l[h] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < HD / 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
+    }
+    __device__ __forceinline__ void chunk(const Params& p, uint32_t stage, int key0, int lane, const unsigned char*, float*) {
+        constexpr int ROW = HD * 2;
+        float s[2][4] = {};
+        const int mi = lane >> 3, r = lane & 7;
+#pragma unroll
+        for (int ks = 0; ks < HD / 16; ++ks) {
+            uint32_t b[4];
+            const int key = (mi >> 1) * 8 + r;
+            ldsm(stage + key * ROW + (((ks * 2 + (mi & 1)) ^ r) << 4), b);
+            mma(s[0], qa[ks], b[0], b[1]);
+            mma(s[1], qa[ks], b[2], b[3]);
+        }
+        float f[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float& x = s[nt][2 * h + e];
+                    x = key0 + nt * 8 + (lane & 3) * 2 + e < lim[h] ? x * p.scale_log2 : -INFINITY;
+                    mx = fmaxf(mx, x);
+                }
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+            const float mn = fmaxf(m[h], mx), ref = mn == -INFINITY ? 0.f : mn;   // (a row that sees nothing yet)
+            f[h] = fast_exp2(m[h] - ref);
+            m[h] = mn;
+            float sum = 0.f;
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float& x = s[nt][2 * h + e];
+                    x = fast_exp2(x - ref);
+                    sum += x;
+                }
+            l[h] = fmaf(l[h], f[h], sum);
+        }
+        if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
+#pragma unroll
+            for (int i = 0; i < HD / 8; ++i) {
+                o[i][0] *= f[0], o[i][1] *= f[0];
+                o[i][2] *= f[1], o[i][3] *= f[1];
+            }
+        }
+        const uint32_t pa[4] = {tc::pack_bf16x2(s[0][0], s[0][1]), tc::pack_bf16x2(s[0][2], s[0][3]),
+                                tc::pack_bf16x2(s[1][0], s[1][1]), tc::pack_bf16x2(s[1][2], s[1][3])};
+        const uint32_t vbase = stage + CK * ROW;
+#pragma unroll
+        for (int np = 0; np < HD / 16; ++np) {
+            uint32_t b[4];
+            const int key = (mi & 1) * 8 + r;
+            ldsm_t(vbase + key * ROW + (((np * 2 + (mi >> 1)) ^ r) << 4), b);
+            mma(o[2 * np], pa, b[0], b[1]);
+            mma(o[2 * np + 1], pa, b[2], b[3]);
+        }
+    }
+    // un-normalised rows to dst [TM][HD], maxima and sums to ml [TM]
+    __device__ __forceinline__ void finish(float* dst, float2* ml, int lane) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float sum = l[h];
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            const int row = lane / 4 + 8 * h;
+            if ((lane & 3) == 0) ml[row] = make_float2(m[h], sum);
+#pragma unroll
+            for (int i = 0; i < HD / 8; ++i)
+                *reinterpret_cast<float2*>(dst + row * HD + i * 8 + (lane & 3) * 2) = make_float2(o[i][2 * h], o[i][2 * h + 1]);
+        }
+    }
+};
+
+template <int HD>
+struct WarpF32 {
+    static constexpr int C = HD / 32;
+    float o[TM][C], m[8], l[8];
+    int lim[8];
+    __device__ __forceinline__ void start(const Params& p, const Unit& u, int lane, const unsigned char*) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int tok = (u.tile * TM + (lane >> 4) * 8 + i) / p.plan.group;
+            lim[i] = tok < u.s.n ? limit_of(p.plan, u.s, tok) : 0;
+            m[i] = -INFINITY;
+            l[i] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[i][c] = 0.f;
+    }
+    __device__ __forceinline__ void chunk(const Params& p, uint32_t, int key0, int lane, const unsigned char* stage, float* qp) {
+        constexpr int ROW = HD * 4;
+        const float* q = qp;                                            // [TM][HD]
+        float* prob = qp + TM * HD + (threadIdx.x >> 5) * CK * TM;      // [CK][TM], this warp's
+        const int key = lane & 15, half = lane >> 4;
+        float s[8] = {};
+#pragma unroll 4
+        for (int c = 0; c < HD / 4; ++c) {
+            const float4 kv = *reinterpret_cast<const float4*>(stage + key * ROW + ((c ^ (key & 7)) << 4));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float4 qv = *reinterpret_cast<const float4*>(q + (half * 8 + i) * HD + c * 4);
+                s[i] = fmaf(kv.x, qv.x, fmaf(kv.y, qv.y, fmaf(kv.z, qv.z, fmaf(kv.w, qv.w, s[i]))));
+            }
+        }
+        float f[8];
+        bool moved = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float x = key0 + key < lim[i] ? s[i] * p.scale_log2 : -INFINITY;
+            float mx = x;
+#pragma unroll
+            for (int d = 8; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+            const float mn = fmaxf(m[i], mx), ref = mn == -INFINITY ? 0.f : mn;
+            f[i] = exp2f(m[i] - ref);
+            moved |= f[i] != 1.f;
+            m[i] = mn;
+            s[i] = exp2f(x - ref);
+            l[i] = fmaf(l[i], f[i], s[i]);   // this lane's key alone, summed over the lanes at the end
+        }
+        __syncwarp();
+        *reinterpret_cast<float4*>(prob + key * TM + half * 8) = make_float4(s[0], s[1], s[2], s[3]);
+        *reinterpret_cast<float4*>(prob + key * TM + half * 8 + 4) = make_float4(s[4], s[5], s[6], s[7]);
+        __syncwarp();
+        if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const float g = __shfl_sync(0xffffffffu, f[i & 7], (i >> 3) * 16);
+#pragma unroll
+                for (int c = 0; c < C; ++c) o[i][c] *= g;
+            }
+        }
+        const unsigned char* v = stage + CK * ROW;
+#pragma unroll 4
+        for (int kk = 0; kk < CK; ++kk) {
+            float vv[C];
+            const int byte = lane * C * 4, piece = byte >> 4;
+            const unsigned char* at = v + kk * ROW + ((piece ^ (kk & 7)) << 4) + (byte & 15);
+            if constexpr (C == 4) {
+                const float4 x = *reinterpret_cast<const float4*>(at);
+                vv[0] = x.x, vv[1] = x.y, vv[2] = x.z, vv[3] = x.w;
+            } else {
+                const float2 x = *reinterpret_cast<const float2*>(at);
+                vv[0] = x.x, vv[1] = x.y;
+            }
+#pragma unroll
+            for (int i4 = 0; i4 < TM / 4; ++i4) {
+                const float4 pr = *reinterpret_cast<const float4*>(prob + kk * TM + i4 * 4);
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    o[i4 * 4][c] = fmaf(pr.x, vv[c], o[i4 * 4][c]);
+                    o[i4 * 4 + 1][c] = fmaf(pr.y, vv[c], o[i4 * 4 + 1][c]);
+                    o[i4 * 4 + 2][c] = fmaf(pr.z, vv[c], o[i4 * 4 + 2][c]);
+                    o[i4 * 4 + 3][c] = fmaf(pr.w, vv[c], o[i4 * 4 + 3][c]);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void finish(float* dst, float2* ml, int lane) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float sum = l[i];
+#pragma unroll
+            for (int d = 8; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            if ((lane & 15) == 0) ml[(lane >> 4) * 8 + i] = make_float2(m[i], sum);
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int c = 0; c < C; ++c) dst[i * HD + lane * C + c] = o[i][c];
+    }
+};
+template <typename T, int HD>
+struct WarpOf { using type = WarpBf16<HD>; };
+template <int HD>
+struct WarpOf<float, HD> { using type = WarpF32<HD>; };
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(kThreads, Geo<T, HD>::CTAS) attend_paged_rows_kernel(const Params p) {
+    using G = Geo<T, HD>;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ long long begin[EC_PAGED_MAX_BATCH + 1];
+    __shared__ float2 ml[kWarps][TM];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    unsigned char* mine = smem + warp * G::WARP;
+    const uint32_t mine_u = tc::s2u(mine);
+    float* qp = reinterpret_cast<float*>(smem + kWarps * G::WARP);
+    tc::pdl_wait();
+    tc::pdl_launch_dependents();
+    lay_out(p.plan, begin);
+    const long long all = begin[p.plan.batch];
+    const int n = workers(p.plan, all, gridDim.x), cta = blockIdx.x;
+    const long long first = cta < n ? cut_of(p.plan, begin, all, n, cta) : all;
+    const long long last = cta < n ? cut_of(p.plan, begin, all, n, cta + 1) : all;
+    if (threadIdx.x == 0) p.cuts[cta] = first;
+    if (threadIdx.x == 0 && cta == 0) p.cuts[gridDim.x] = all;
+
+    for (long long w = first; w < last;) {
+        const Unit u = unit_at(p.plan, begin, w);
+        const int j0 = (int)(w - u.w0), j1 = (int)min((long long)u.steps, last - u.w0);
+        w = u.w0 + j1;
+        const long long rows_all = (long long)u.s.n * p.plan.group;
+        const int32_t* table = p.page_table + (long long)u.b * p.max_pages;
+        const long long page_rows = (long long)p.plan.n_kv_heads << p.page_shift;
+        // a lane's part of a chunk: 16-byte piece `piece` of rows lane / LR, + RW, ...
+        constexpr int PIECES = HD * (int)sizeof(T) / 16, RW = 32 / (PIECES < 32 ? PIECES : 32), LR = PIECES < 32 ? PIECES : 32;
+        auto page_at = [&](int j) -> int {
+            const int key0 = j * TK + warp * CK;
+            return j < j1 && key0 < u.s.kv ? table[key0 >> p.page_shift] : -1;
+        };
+        auto issue = [&](int j, int page) {
+            if (j < j1) {
+                const int key0 = j * TK + warp * CK, slot = (j - j0) % kStages;
+                int valid = min(u.s.kv - key0, CK);
+                if (valid > 0 && (unsigned)page >= (unsigned)p.n_pages) {
+                    if (lane == 0 && p.plan.dev_status) atomicExch(p.plan.dev_status, (int)EC_ERR_PAGE);
+                    valid = 0;
+                }
+                const long long row = (valid > 0 ? page : 0) * page_rows + ((long long)u.head << p.page_shift) + (key0 & ((1 << p.page_shift) - 1));
+                const uint32_t dst = mine_u + slot * G::STAGE;
+                const unsigned char* ks = static_cast<const unsigned char*>(p.k) + (valid > 0 ? row : 0) * (HD * (long long)sizeof(T));
+                const unsigned char* vs = static_cast<const unsigned char*>(p.v) + (valid > 0 ? row : 0) * (HD * (long long)sizeof(T));
+#pragma unroll
+                for (int i = 0; i < CK / RW; ++i) {
+                    const int r = i * RW + lane / LR, piece = lane % LR;
+                    const bool ok = r < valid;
+                    const int off = ok ? r * HD * (int)sizeof(T) + piece * 16 : 0;   // (an address inside the pool in any case)
+                    const uint32_t to = dst + r * HD * (int)sizeof(T) + ((piece ^ (r & 7)) << 4);
+                    cp16(to, ks + off, ok);
+                    cp16(to + G::CHUNK, vs + off, ok);
+                }
+            }
+            cp_commit();
+        };
+        int page = page_at(j0);
+        for (int i = 0; i < kStages - 1; ++i) {
+            const int next = page_at(j0 + i + 1);
+            issue(j0 + i, page);
+            page = next;
+        }
+        if constexpr (sizeof(T) == 4) {
+            for (int i = threadIdx.x; i < TM * HD / 4; i += kThreads) {
+                const int r = i / (HD / 4), c = i % (HD / 4), pr = u.tile * TM + r, tok = pr / p.plan.group;
+                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (tok < u.s.n)
+                    x = *reinterpret_cast<const float4*>(static_cast<const float*>(p.q) +
+                        ((long long)(u.s.row0 + tok) * p.n_q_heads + u.head * p.plan.group + pr % p.plan.group) * HD + c * 4);
+                *reinterpret_cast<float4*>(qp + r * HD + c * 4) = x;
+            }
+            __syncthreads();
+        }
+        typename WarpOf<T, HD>::type state;
+        state.start(p, u, lane, mine);
+        for (int j = j0; j < j1; ++j) {
+            const int next = page_at(j + kStages);
+            issue(j + kStages - 1, page);
+            page = next;
+            cp_wait<kStages - 1>();
+            __syncwarp();
+            const int slot = (j - j0) % kStages, key0 = j * TK + warp * CK;
+            if (key0 < u.s.kv) state.chunk(p, mine_u + slot * G::STAGE, key0, lane, mine + slot * G::STAGE, qp);
+            __syncwarp();   // the slot is free for the load after next
+        }
+        cp_wait<0>();
+        __syncwarp();
+        state.finish(reinterpret_cast<float*>(mine), ml[warp], lane);
+        __syncthreads();
+        const bool whole = j0 == 0 && j1 == u.steps;
+        float* part = p.partial + ((long long)cta * 2 + (j0 == 0 ? 1 : 0)) * (TM * (HD + 2));
+        for (int i = threadIdx.x; i < TM * HD / 4; i += kThreads) {
+            const int r = i / (HD / 4), c = i % (HD / 4) * 4;
+            const long long pr = (long long)u.tile * TM + r;
+            float M = -INFINITY, L = 0.f;
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) M = fmaxf(M, ml[k][r].x);
+            const float ref = M == -INFINITY ? 0.f : M;
+            float acc[4] = {};
+#pragma unroll
+            for (int k = 0; k < kWarps; ++k) {
+                const float f = exp2f(ml[k][r].x - ref);
+                L = fmaf(f, ml[k][r].y, L);
+                const float4 x = *reinterpret_cast<const float4*>(smem + k * G::WARP + (r * HD + c) * 4);
+                acc[0] = fmaf(f, x.x, acc[0]), acc[1] = fmaf(f, x.y, acc[1]);
+                acc[2] = fmaf(f, x.z, acc[2]), acc[3] = fmaf(f, x.w, acc[3]);
+            }
+            if (!whole) {
+                *reinterpret_cast<float4*>(part + r * HD + c) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+                if (c == 0) *reinterpret_cast<float2*>(part + TM * HD + r * 2) = make_float2(M, L);
+            } else if (pr < rows_all) {
+                const float inv = L > 0.f ? 1.f / L : 0.f;
+                T* dst = static_cast<T*>(p.out) + ((u.s.row0 + pr / p.plan.group) * p.n_q_heads + u.head * p.plan.group + pr % p.plan.group) * HD + c;
+                store4(dst, acc, inv);
+            }
+        }
+        __syncthreads();   // before the next unit's loads and rows
+    }
+}
+
+template <typename T, int HD>
+cudaError_t launch(const PagedArgs& a, cudaStream_t stream) {
+    using G = Geo<T, HD>;
+    Params p;
+    p.plan = make_plan(a, TM, TK);
+    p.plan.min_steps = 2;
+    p.q = a.q, p.k = a.k_pages, p.v = a.v_pages, p.out = a.out;
+    p.page_table = a.page_table;
+    p.page_shift = __builtin_ctz((unsigned)a.d.page_size);
+    p.n_pages = a.d.n_pages, p.max_pages = a.d.max_pages, p.n_q_heads = a.d.n_q_heads;
+    p.scale_log2 = a.scale * kLog2e;
+    const int ctas = sm_count() * G::CTAS;
+    p.cuts = static_cast<long long*>(a.workspace);
+    p.partial = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + cuts_bytes(ctas));
+    static PerDeviceOnce once;
+    if (const cudaError_t e = ensure_dynamic_smem(once, attend_paged_rows_kernel<T, HD>, G::BYTES); e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(ctas, 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = G::BYTES;
+    cfg.stream = stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (const cudaError_t e = cudaLaunchKernelEx(&cfg, attend_paged_rows_kernel<T, HD>, p); e != cudaSuccess) return e;
+    return launch_combine<T, HD>(p.plan, p.cuts, p.partial, a.out, a.d.n_q_heads, ctas, stream);
+}
+
+}  // namespace
+
+size_t attend_paged_rows_workspace(const ec_paged_desc& d) {
+    const int ctas = sm_count() * 4;   // at most
+    return cuts_bytes(ctas) + (size_t)ctas * 2 * TM * (d.head_dim + 2) * 4;
+}
+
+cudaError_t launch_attend_paged_rows(const PagedArgs& a, cudaStream_t stream) {
+    if (a.d.dtype == EC_BF16)
+        return a.d.head_dim == 128 ? launch<__nv_bfloat16, 128>(a, stream) : launch<__nv_bfloat16, 64>(a, stream);
+    return a.d.head_dim == 128 ? launch<float, 128>(a, stream) : launch<float, 64>(a, stream);
+}
+
+}  // namespace ec

@@ -160,4 +160,70 @@ cudaError_t launch_attend_dense(const AttendArgs& a, cudaStream_t stream);
 size_t attend_tc_workspace_bytes(const ec_attn_desc& d, int n_active);
 cudaError_t launch_attend_bf16_tc(const AttendArgs& a, cudaStream_t stream);   // tcgen05 path (head_dim 128)
 
+// ---- paged cache, rotation, sampling ----
+struct RopeArgs {
+    ec_rope_desc d;
+    const void *q, *k, *v;
+    long long q_stride, k_stride, v_stride;   // elements between rows
+    const void *q_weight, *k_weight;
+    const int32_t* positions;
+    const float* inv_freq;
+    int n_rows;
+    void* q_out;
+    void* k_out;   // dense [n_rows, n_kv_heads, head_dim], or the K pages
+    // paged form
+    void* v_pages = nullptr;
+    const int32_t* row_offsets = nullptr;
+    const int32_t* page_table = nullptr;
+    int batch = 0, page_size = 0, n_pages = 0, max_pages = 0;
+    int32_t* dev_status = nullptr;
+};
+cudaError_t launch_rope(const RopeArgs& a, cudaStream_t stream);
+
+struct PagedArgs {
+    ec_paged_desc d;
+    const void* q;
+    const int32_t* row_offsets;
+    const int32_t* kv_lens;
+    int n_rows, max_rows;
+    const int32_t* page_table;
+    const void* k_pages;
+    const void* v_pages;
+    void* out;
+    void* workspace;
+    int32_t* dev_status;
+    float scale;   // resolved (never 0)
+};
+size_t attend_paged_rows_workspace(const ec_paged_desc& d);
+cudaError_t launch_attend_paged_rows(const PagedArgs& a, cudaStream_t stream);
+
+cudaError_t launch_pages_fork(const ec_pages_desc& d, int32_t* table, int32_t* lens, int32_t* refs, const int32_t* src,
+                              const int32_t* dst, int n, int32_t* dev_status, cudaStream_t stream);
+cudaError_t launch_pages_reserve(const ec_pages_desc& d, int32_t* table, int32_t* lens, int32_t* refs,
+                                 const int32_t* write_from, const int32_t* new_lens, int32_t* copy_src, int32_t* copy_dst,
+                                 int copy_cap, int32_t* n_copies, void* workspace, int32_t* dev_status, cudaStream_t stream);
+cudaError_t launch_pages_release(const ec_pages_desc& d, int32_t* table, int32_t* lens, int32_t* refs,
+                                 const int32_t* keep_lens, cudaStream_t stream);
+cudaError_t launch_pages_compact(const ec_pages_desc& d, int32_t* table, const int32_t* lens, int32_t* refs, int32_t* copy_src,
+                                 int32_t* copy_dst, int copy_cap, int32_t* n_copies, void* workspace, cudaStream_t stream);
+size_t pages_workspace_bytes(int n_pages);
+cudaError_t launch_pages_copy(void* k_pages, void* v_pages, long long page_bytes, int n_pages, int n_layers,
+                              long long layer_bytes, const int32_t* src, const int32_t* dst, int cap,
+                              const int32_t* n_copies, int32_t* dev_status, cudaStream_t stream);
+
+struct SampleArgs {
+    const void* logits;
+    int dtype, n_rows, vocab;
+    long long row_stride;
+    const float *u, *temperature;
+    const int32_t* top_k;
+    const float *top_p, *min_p;
+    int32_t* token_out;
+    float* prob_out;
+    int32_t* kept_out;
+    void* workspace;
+};
+size_t sample_workspace_bytes(int n_rows, int vocab);
+cudaError_t launch_sample(const SampleArgs& a, cudaStream_t stream);
+
 }  // namespace ec

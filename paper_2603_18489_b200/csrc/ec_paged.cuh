@@ -1,0 +1,166 @@
+// How the attention kernels over pages cut their work, on the device: nothing about lengths is known on the host.
+//
+// The query rows of a kv head (rows of the sequence x its H_q / H_kv query heads, "packed", the query head fastest) are
+// taken in tiles of `tm`; a unit is one tile of one kv head of one sequence and takes as many steps as there are key
+// tiles of `tk` keys below the highest limit of its rows (one step where it sees nothing: the zeros are written there).
+// All units' steps, in the order (sequence, kv head, row tile), form one line that is cut into equal pieces, one for
+// each CTA.  A unit that a cut divides leaves un-normalised partial rows in the workspace, which a second launch joins:
+// every CTA has at most one unit that began before it (slot 0) and one that goes on behind it (slot 1).
+#pragma once
+
+#include "ec_common.cuh"
+
+namespace ec {
+namespace paged {
+
+struct Plan {
+    const int32_t* row_offsets;
+    const int32_t* kv_lens;
+    int batch, n_rows, max_rows, max_kv;
+    int group, n_kv_heads, mask_block;
+    int tm, tk;
+    int min_steps;   // a CTA is given at least this many steps, fewer CTAs work where there are not enough
+    int32_t* dev_status;
+};
+
+struct Seq {
+    int row0, n, kv;
+};
+__device__ __forceinline__ Seq seq_of(const Plan& p, int b) {
+    const int r0 = min(max(p.row_offsets[b], 0), p.n_rows), r1 = min(max(p.row_offsets[b + 1], r0), p.n_rows);
+    return Seq{r0, min(r1 - r0, p.max_rows), min(max(p.kv_lens[b], 0), p.max_kv)};
+}
+__device__ __forceinline__ bool seq_is_cut(const Plan& p, int b, const Seq& s) {
+    return p.row_offsets[b + 1] - p.row_offsets[b] != s.n || p.kv_lens[b] != s.kv;
+}
+// keys that row i of the sequence sees
+__device__ __forceinline__ int limit_of(const Plan& p, const Seq& s, int i) {
+    if (p.mask_block == 0) return s.kv;
+    const int pos = s.kv - s.n + i;
+    if (pos < 0) return 0;
+    const long long lim = ((long long)(pos / p.mask_block) + 1) * p.mask_block;
+    return lim < s.kv ? (int)lim : s.kv;
+}
+__device__ __forceinline__ int tiles_of(const Plan& p, const Seq& s) {
+    return (int)(((long long)s.n * p.group + p.tm - 1) / p.tm);
+}
+// steps of row tile `rt` (limits ascend with the row, so the last row of the tile has the highest)
+__device__ __forceinline__ int steps_of(const Plan& p, const Seq& s, int rt) {
+    const long long last = min((long long)(rt + 1) * p.tm, (long long)s.n * p.group) - 1;
+    const int lim = limit_of(p, s, (int)(last / p.group));
+    return max(1, (lim + p.tk - 1) / p.tk);
+}
+
+struct Unit {
+    int b, head, tile;
+    Seq s;
+    long long w0;   // first step on the line
+    int steps;
+};
+
+// begin[b] = first step of sequence b on the line, begin[batch] = all of them; called by the whole CTA
+__device__ __forceinline__ void lay_out(const Plan& p, long long* begin) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    if (p.mask_block == 0) {
+        for (int b = threadIdx.x; b < p.batch; b += blockDim.x) {
+            const Seq s = seq_of(p, b);
+            begin[b + 1] = s.n > 0 ? (long long)tiles_of(p, s) * steps_of(p, s, 0) * p.n_kv_heads : 0;
+        }
+    } else {
+        for (int b = warp; b < p.batch; b += warps) {
+            const Seq s = seq_of(p, b);
+            const int tiles = tiles_of(p, s);
+            long long sum = 0;
+            for (int t = lane; t < tiles; t += 32) sum += steps_of(p, s, t);
+#pragma unroll
+            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (lane == 0) begin[b + 1] = sum * p.n_kv_heads;
+        }
+    }
+    if (p.dev_status && blockIdx.x == 0)
+        for (int b = threadIdx.x; b < p.batch; b += blockDim.x)
+            if (seq_is_cut(p, b, seq_of(p, b))) atomicExch(p.dev_status, (int)EC_ERR_SHAPE);
+    __syncthreads();
+    if (warp == 0) {
+        long long carry = 0;
+        for (int b0 = 0; b0 < p.batch; b0 += 32) {
+            long long v = b0 + lane < p.batch ? begin[b0 + lane + 1] : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long u = __shfl_up_sync(0xffffffffu, v, o);
+                if (lane >= o) v += u;
+            }
+            if (b0 + lane < p.batch) begin[b0 + lane + 1] = carry + v;
+            carry += __shfl_sync(0xffffffffu, v, 31);
+        }
+        if (lane == 0) begin[0] = 0;
+    }
+    __syncthreads();
+}
+
+// the unit that step `w` (0 <= w < all) belongs to; called by whole warps, every lane gets it
+__device__ __forceinline__ Unit unit_at(const Plan& p, const long long* begin, long long w) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = p.batch - 1;   // the last sequence that begins at or before w (empty ones end where they begin)
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (begin[mid] <= w) lo = mid; else hi = mid - 1;
+    }
+    Unit u;
+    u.b = lo;
+    u.s = seq_of(p, lo);
+    const long long per_head = (begin[lo + 1] - begin[lo]) / p.n_kv_heads, at = w - begin[lo];
+    u.head = (int)(at / per_head);
+    const long long in_head = at - u.head * per_head, head0 = begin[lo] + u.head * per_head;
+    if (p.mask_block == 0) {
+        u.steps = steps_of(p, u.s, 0);
+        u.tile = (int)(in_head / u.steps);
+        u.w0 = head0 + (long long)u.tile * u.steps;
+        return u;
+    }
+    const int tiles = tiles_of(p, u.s);
+    long long done = 0;
+    u.tile = 0, u.steps = 1, u.w0 = head0;
+    for (int t0 = 0; t0 < tiles; t0 += 32) {
+        const int mine = t0 + lane < tiles ? steps_of(p, u.s, t0 + lane) : 0;
+        int run = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, run, o);
+            if (lane >= o) run += x;
+        }
+        const uint32_t past = __ballot_sync(0xffffffffu, done + run > in_head);
+        if (past) {
+            const int first = __ffs(past) - 1;
+            u.tile = t0 + first;
+            u.steps = __shfl_sync(0xffffffffu, mine, first);
+            u.w0 = head0 + done + __shfl_sync(0xffffffffu, run, first) - u.steps;
+            break;
+        }
+        done += __shfl_sync(0xffffffffu, run, 31);
+    }
+    return u;
+}
+
+// CTAs that get work
+__device__ __forceinline__ int workers(const Plan& p, long long all, int ctas) {
+    const long long n = (all + p.min_steps - 1) / p.min_steps;
+    return (int)min((long long)ctas, max(n, 1ll));
+}
+// first step of CTA c of `n`.  A cut that would leave a quarter of its unit or less on one side is moved to that end of the unit
+// where the steps allow it (the partial rows of a unit cost about as much as a step).
+__device__ __forceinline__ long long cut_of(const Plan& p, const long long* begin, long long all, int n, int c) {
+    if (c <= 0) return 0;
+    if (c >= n) return all;
+    const long long w = all / n * c + all % n * c / n;
+    const Unit u = unit_at(p, begin, w);
+    const int in = (int)(w - u.w0);
+    if (in == 0) return w;
+    const int slack = u.steps / 4 < p.min_steps / 2 ? u.steps / 4 : p.min_steps / 2;
+    if (in <= slack) return u.w0;
+    if (u.steps - in <= slack) return u.w0 + u.steps;
+    return w;
+}
+
+}  // namespace paged
+}  // namespace ec

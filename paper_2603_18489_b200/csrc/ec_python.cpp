@@ -11,6 +11,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -398,10 +399,297 @@ PyObject* select_recent_sliding(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- paged cache, rotation, sampling -------------------------------------------------------------------------------
+// The tensors of one call: checked one by one, all on one GPU, which is the current device while the call is made.
+class Call {
+public:
+    const at::Tensor& cuda(PyObject* o, const char* name) {
+        const at::Tensor& t = tensor(o, name);
+        if (!t.is_cuda()) raise(PyExc_ValueError, std::string(name) + " must be a CUDA tensor (the library has no host path)");
+        if (device_ >= 0 && t.device().index() != device_)
+            raise(PyExc_ValueError, std::string(name) + " is on another device than the tensors before it");
+        device_ = t.device().index();
+        return t;
+    }
+    // a dense tensor of `type` with `n` elements (n < 0: any number); nullptr for None where that is allowed
+    void* dense(PyObject* o, const char* name, at::ScalarType type, int64_t n, bool optional = false) {
+        if (o == Py_None && optional) return nullptr;
+        const at::Tensor& t = cuda(o, name);
+        if (!t.is_contiguous()) raise(PyExc_ValueError, std::string(name) + " must be contiguous");
+        if (t.scalar_type() != type) raise(PyExc_TypeError, std::string(name) + " must be " + c10::toString(type));
+        if (n >= 0 && t.numel() != n)
+            raise(PyExc_ValueError, std::string(name) + " must hold " + std::to_string(n) + " elements, it holds " + std::to_string(t.numel()));
+        return t.data_ptr();
+    }
+    int32_t* ints(PyObject* o, const char* name, int64_t n, bool optional = false) {
+        return static_cast<int32_t*>(dense(o, name, at::kInt, n, optional));
+    }
+    float* floats(PyObject* o, const char* name, int64_t n, bool optional = false) {
+        return static_cast<float*>(dense(o, name, at::kFloat, n, optional));
+    }
+    void* workspace(PyObject* o, size_t* bytes) {
+        *bytes = bytes_of(o);
+        if (o == Py_None) return nullptr;
+        const at::Tensor& t = cuda(o, "workspace");
+        if (!t.is_contiguous()) raise(PyExc_ValueError, "workspace must be contiguous");
+        return t.data_ptr();
+    }
+    // [rows, heads, dim] whose heads are contiguous; rows may be apart.  Returns the pointer, sets the stride.
+    void* rows(PyObject* o, const char* name, at::ScalarType type, int64_t n_rows, int64_t heads, int64_t dim, int64_t* stride) {
+        const at::Tensor& t = cuda(o, name);
+        if (t.scalar_type() != type) raise(PyExc_TypeError, std::string(name) + " must be " + c10::toString(type));
+        const int64_t d = t.dim();
+        if (d < 3 || t.size(d - 1) != dim || t.size(d - 2) != heads) raise(PyExc_ValueError, std::string(name) + " must be [rows, heads, head_dim]");
+        if (t.numel() != n_rows * heads * dim) raise(PyExc_ValueError, std::string(name) + " must have one row for each row of q");
+        if ((dim > 1 && t.stride(d - 1) != 1) || (heads > 1 && t.stride(d - 2) != dim))
+            raise(PyExc_ValueError, std::string("the heads of a row of ") + name + " must be contiguous");
+        *stride = heads * dim;
+        if (d == 3) {
+            if (t.size(0) > 1) *stride = t.stride(0);
+        } else if (!t.is_contiguous()) {
+            raise(PyExc_ValueError, std::string(name) + " must be contiguous or [rows, heads, head_dim]");
+        }
+        return t.data_ptr();
+    }
+    void* stream(PyObject* o) const {
+        if (o != Py_None) return stream_of(o);
+        return device_ >= 0 ? c10::cuda::getCurrentCUDAStream(device_).stream() : c10::cuda::getCurrentCUDAStream().stream();
+    }
+    template <class F>
+    PyObject* run(F f) const {
+        c10::cuda::OptionalCUDAGuard guard;
+        if (device_ >= 0) guard.set_index(device_);
+        return PyLong_FromLong(without_gil(f));
+    }
+
+private:
+    c10::DeviceIndex device_ = -1;
+};
+template <class D>
+D host_struct(PyObject* o, const char* what) {
+    Py_buffer v;
+    if (PyObject_GetBuffer(o, &v, PyBUF_SIMPLE) != 0) throw PyRaised();
+    D d;
+    const bool ok = v.len == (Py_ssize_t)sizeof d;
+    if (ok) d = *static_cast<const D*>(v.buf);
+    PyBuffer_Release(&v);
+    if (!ok) raise(PyExc_TypeError, std::string("desc must be an ") + what);
+    return d;
+}
+at::ScalarType element_of(int32_t dtype) { return dtype == EC_BF16 ? at::kBFloat16 : at::kFloat; }
+int64_t pool_elements(const ec_paged_desc& d) { return (int64_t)d.n_pages * d.n_kv_heads * d.page_size * d.head_dim; }
+int64_t rows_of(PyObject* o, const char* name, int64_t heads, int64_t dim) {
+    const at::Tensor& t = tensor(o, name);
+    if (heads < 1 || dim < 1) return 0;   // the library refuses the descriptor
+    const int64_t n = t.numel() / (heads * dim);
+    if (n > INT32_MAX) raise(PyExc_OverflowError, std::string(name) + " has too many rows");
+    return n;
+}
+
+// (desc, q, row_offsets, kv_lens, max_rows, page_table, k_pages, v_pages, out, workspace, dev_status, stream)
+PyObject* attend_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n, 12);
+        const auto d = host_struct<ec_paged_desc>(a[0], "ec_paged_desc");
+        const at::ScalarType e = element_of(d.dtype);
+        Call c;
+        const int64_t rows = rows_of(a[1], "q", d.n_q_heads, d.head_dim), all = rows * d.n_q_heads * d.head_dim;
+        const void* q = c.dense(a[1], "q", e, all);
+        const int32_t *ro = c.ints(a[2], "row_offsets", (int64_t)d.batch + 1), *kl = c.ints(a[3], "kv_lens", d.batch);
+        const int32_t max_rows = int32(a[4]);
+        const int32_t* pt = c.ints(a[5], "page_table", (int64_t)d.batch * d.max_pages);
+        const void *kp = c.dense(a[6], "k_pages", e, pool_elements(d)), *vp = c.dense(a[7], "v_pages", e, pool_elements(d));
+        void* out = c.dense(a[8], "out", e, all);
+        size_t ws_bytes;
+        void* ws = c.workspace(a[9], &ws_bytes);
+        int32_t* status = c.ints(a[10], "dev_status", -1, true);
+        void* s = c.stream(a[11]);
+        return c.run([&] {
+            return ec_attend_paged(&d, q, ro, kl, (int32_t)rows, max_rows, pt, kp, vp, out, ws, ws_bytes, status, s);
+        });
+    });
+}
+
+// (desc, q, k, q_weight, k_weight, positions, inv_freq, q_out, k_out, stream)
+PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n, 10);
+        const auto d = host_struct<ec_rope_desc>(a[0], "ec_rope_desc");
+        const at::ScalarType e = element_of(d.dtype);
+        Call c;
+        const int64_t rows = rows_of(a[1], "q", d.n_q_heads, d.head_dim);
+        int64_t qs, ks;
+        const void *q = c.rows(a[1], "q", e, rows, d.n_q_heads, d.head_dim, &qs), *k = c.rows(a[2], "k", e, rows, d.n_kv_heads, d.head_dim, &ks);
+        const void *qw = c.dense(a[3], "q_weight", e, d.head_dim, true), *kw = c.dense(a[4], "k_weight", e, d.head_dim, true);
+        const int32_t* pos = c.ints(a[5], "positions", rows);
+        const float* f = c.floats(a[6], "inv_freq", d.rot_dim / 2, true);
+        void *qo = c.dense(a[7], "q_out", e, rows * d.n_q_heads * d.head_dim), *ko = c.dense(a[8], "k_out", e, rows * d.n_kv_heads * d.head_dim);
+        void* s = c.stream(a[9]);
+        return c.run([&] { return ec_qk_norm_rope(&d, q, qs, k, ks, qw, kw, pos, f, (int32_t)rows, qo, ko, s); });
+    });
+}
+
+// (desc, paged, q, k, v, q_weight, k_weight, row_offsets, positions, inv_freq, page_table, q_out, k_pages, v_pages,
+//  dev_status, stream)
+PyObject* qk_norm_rope_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n, 16);
+        const auto d = host_struct<ec_rope_desc>(a[0], "ec_rope_desc");
+        const auto g = host_struct<ec_paged_desc>(a[1], "ec_paged_desc");
+        const at::ScalarType e = element_of(d.dtype);
+        Call c;
+        const int64_t rows = rows_of(a[2], "q", d.n_q_heads, d.head_dim);
+        int64_t qs, ks, vs;
+        const void *q = c.rows(a[2], "q", e, rows, d.n_q_heads, d.head_dim, &qs), *k = c.rows(a[3], "k", e, rows, d.n_kv_heads, d.head_dim, &ks),
+                   *v = c.rows(a[4], "v", e, rows, d.n_kv_heads, d.head_dim, &vs);
+        const void *qw = c.dense(a[5], "q_weight", e, d.head_dim, true), *kw = c.dense(a[6], "k_weight", e, d.head_dim, true);
+        const int32_t *ro = c.ints(a[7], "row_offsets", (int64_t)g.batch + 1), *pos = c.ints(a[8], "positions", rows);
+        const float* f = c.floats(a[9], "inv_freq", d.rot_dim / 2, true);
+        const int32_t* pt = c.ints(a[10], "page_table", (int64_t)g.batch * g.max_pages);
+        void *qo = c.dense(a[11], "q_out", e, rows * d.n_q_heads * d.head_dim), *kp = c.dense(a[12], "k_pages", e, pool_elements(g)),
+             *vp = c.dense(a[13], "v_pages", e, pool_elements(g));
+        int32_t* status = c.ints(a[14], "dev_status", -1, true);
+        void* s = c.stream(a[15]);
+        return c.run([&] {
+            return ec_qk_norm_rope_paged(&d, &g, q, qs, k, ks, v, vs, qw, kw, ro, pos, f, (int32_t)rows, pt, qo, kp, vp, status, s);
+        });
+    });
+}
+
+// (logits, vocab, u, temperature, top_k, top_p, min_p, token, prob, kept, workspace, stream)
+PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n, 12);
+        Call c;
+        const at::Tensor& t = c.cuda(a[0], "logits");
+        if (t.dim() != 2) raise(PyExc_ValueError, "logits must be a 2-D CUDA tensor [n_rows, row_stride]");
+        if (t.size(1) > 1 && t.stride(1) != 1) raise(PyExc_ValueError, "logits rows must be contiguous");
+        const int32_t type = dtype_code(t), rows = (int32_t)t.size(0), vocab = int32(a[1]);
+        if (vocab > t.size(1)) raise(PyExc_ValueError, "logits rows hold fewer than vocab columns");
+        const int64_t stride = rows > 1 ? t.stride(0) : (t.size(1) + 7) / 8 * 8;   // (of one row the stride is not used)
+        const float *u = c.floats(a[2], "u", rows), *temp = c.floats(a[3], "temperature", rows, true);
+        const int32_t* top_k = c.ints(a[4], "top_k", rows, true);
+        const float *top_p = c.floats(a[5], "top_p", rows, true), *min_p = c.floats(a[6], "min_p", rows, true);
+        int32_t* token = c.ints(a[7], "token_out", rows);
+        float* prob = c.floats(a[8], "prob_out", rows, true);
+        int32_t* kept = c.ints(a[9], "kept_out", rows, true);
+        size_t ws_bytes;
+        void* ws = c.workspace(a[10], &ws_bytes);
+        void* s = c.stream(a[11]);
+        const void* lg = t.data_ptr();
+        return c.run([&] {
+            return ec_sample(lg, type, rows, vocab, stride, u, temp, top_k, top_p, min_p, token, prob, kept, ws, ws_bytes, s);
+        });
+    });
+}
+
+// the state of the pages: (page_table [B, M], kv_lens [B], ref_counts [P]), page_size
+struct PagesState {
+    ec_pages_desc d;
+    int32_t *table, *lens, *refs;
+    PagesState(Call& c, PyObject* const* a, PyObject* page_size) {
+        const at::Tensor& t = c.cuda(a[0], "page_table");
+        if (t.dim() != 2) raise(PyExc_ValueError, "page_table must be int32 [batch, max_pages]");
+        const at::Tensor& r = c.cuda(a[2], "ref_counts");
+        if (t.size(0) > INT32_MAX || t.size(1) > INT32_MAX || r.numel() > INT32_MAX) raise(PyExc_OverflowError, "too many pages");
+        d.batch = (int32_t)t.size(0), d.max_pages = (int32_t)t.size(1), d.n_pages = (int32_t)r.numel(), d.page_size = int32(page_size);
+        table = c.ints(a[0], "page_table", -1);
+        lens = c.ints(a[1], "kv_lens", d.batch);
+        refs = c.ints(a[2], "ref_counts", d.n_pages);
+    }
+};
+int32_t cap_of(PyObject* src, PyObject* dst) {
+    const int64_t n = tensor(src, "copy_src").numel();
+    if (n > INT32_MAX || tensor(dst, "copy_dst").numel() != n) raise(PyExc_ValueError, "copy_src and copy_dst must have the same length");
+    return (int32_t)n;
+}
+
+// (page_table, kv_lens, ref_counts, page_size, src, dst, dev_status, stream)
+PyObject* pages_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n, 8);
+        Call c;
+        const PagesState p(c, a, a[3]);
+        const int64_t k = tensor(a[4], "src").numel();
+        const int32_t *src = c.ints(a[4], "src", k), *dst = c.ints(a[5], "dst", k);
+        if (k > INT32_MAX) raise(PyExc_OverflowError, "too many pairs");
+        int32_t* status = c.ints(a[6], "dev_status", -1, true);
+        void* s = c.stream(a[7]);
+        return c.run([&] { return ec_pages_fork(&p.d, p.table, p.lens, p.refs, src, dst, (int32_t)k, status, s); });
+    });
+}
+// (page_table, kv_lens, ref_counts, page_size, write_from, new_lens, copy_src, copy_dst, n_copies, workspace, dev_status, stream)
+PyObject* pages_reserve(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n, 12);
+        Call c;
+        const PagesState p(c, a, a[3]);
+        const int32_t *from = c.ints(a[4], "write_from", p.d.batch), *now = c.ints(a[5], "new_lens", p.d.batch);
+        const int32_t cap = cap_of(a[6], a[7]);
+        int32_t *src = c.ints(a[6], "copy_src", cap), *dst = c.ints(a[7], "copy_dst", cap), *count = c.ints(a[8], "n_copies", 1);
+        size_t ws_bytes;
+        void* ws = c.workspace(a[9], &ws_bytes);
+        int32_t* status = c.ints(a[10], "dev_status", -1, true);
+        void* s = c.stream(a[11]);
+        return c.run([&] {
+            return ec_pages_reserve(&p.d, p.table, p.lens, p.refs, from, now, src, dst, cap, count, ws, ws_bytes, status, s);
+        });
+    });
+}
+// (page_table, kv_lens, ref_counts, page_size, keep_lens, stream)
+PyObject* pages_release(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n, 6);
+        Call c;
+        const PagesState p(c, a, a[3]);
+        const int32_t* keep = c.ints(a[4], "keep_lens", p.d.batch);
+        void* s = c.stream(a[5]);
+        return c.run([&] { return ec_pages_release(&p.d, p.table, p.lens, p.refs, keep, s); });
+    });
+}
+// (page_table, kv_lens, ref_counts, page_size, copy_src, copy_dst, n_copies, workspace, stream)
+PyObject* pages_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n, 9);
+        Call c;
+        const PagesState p(c, a, a[3]);
+        const int32_t cap = cap_of(a[4], a[5]);
+        int32_t *src = c.ints(a[4], "copy_src", cap), *dst = c.ints(a[5], "copy_dst", cap), *count = c.ints(a[6], "n_copies", 1);
+        size_t ws_bytes;
+        void* ws = c.workspace(a[7], &ws_bytes);
+        void* s = c.stream(a[8]);
+        return c.run([&] { return ec_pages_compact(&p.d, p.table, p.lens, p.refs, src, dst, cap, count, ws, ws_bytes, s); });
+    });
+}
+// (k_pages, v_pages, copy_src, copy_dst, n_copies, layered, dev_status, stream): pools [n_pages, ...] or, layered, [n_layers, n_pages, ...]
+PyObject* pages_copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n, 8);
+        Call c;
+        const at::Tensor &k = c.cuda(a[0], "k_pages"), &v = c.cuda(a[1], "v_pages");
+        const bool layered = PyObject_IsTrue(a[5]) == 1;
+        const int64_t lead = layered ? 2 : 1;
+        if (k.dim() <= lead || !k.is_contiguous() || !v.is_contiguous() || k.sizes() != v.sizes() || k.scalar_type() != v.scalar_type())
+            raise(PyExc_ValueError, "k_pages and v_pages must be contiguous and alike: [n_pages, ...] or [n_layers, n_pages, ...]");
+        const int64_t layers = layered ? k.size(0) : 1, pages = k.size(lead - 1);
+        if (layers > INT32_MAX || pages > INT32_MAX) raise(PyExc_OverflowError, "too many pages");
+        const int64_t bytes = layers * pages > 0 ? (int64_t)k.nbytes() / (layers * pages) : 0;
+        const int32_t cap = cap_of(a[2], a[3]);
+        const int32_t *src = c.ints(a[2], "copy_src", cap), *dst = c.ints(a[3], "copy_dst", cap), *count = c.ints(a[4], "n_copies", 1, true);
+        int32_t* status = c.ints(a[6], "dev_status", -1, true);
+        void *s = c.stream(a[7]), *kp = k.data_ptr(), *vp = v.data_ptr();
+        return c.run([&] {
+            return ec_pages_copy(kp, vp, bytes, (int32_t)pages, (int32_t)layers, bytes * pages, src, dst, cap, count, status, s);
+        });
+    });
+}
+
 #define EC_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {EC_FAST(kv_refresh),   EC_FAST(attend),        EC_FAST(gate),
                          EC_FAST(gate_decode),  EC_FAST(gate_metrics),  EC_FAST(select_recent),
-                         EC_FAST(select_recent_sliding), {nullptr, nullptr, 0, nullptr}};
+                         EC_FAST(select_recent_sliding), EC_FAST(attend_paged), EC_FAST(qk_norm_rope),
+                         EC_FAST(qk_norm_rope_paged), EC_FAST(sample), EC_FAST(pages_fork), EC_FAST(pages_reserve),
+                         EC_FAST(pages_release), EC_FAST(pages_compact), EC_FAST(pages_copy), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_ec_python", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,528 @@
+// ec_sample: one token per logits row from temperature, top-k, top-p, min-p and a given uniform number.
+//
+// With the tokens ordered by (logit, descending; index, ascending) every filter keeps a prefix, so a row is three searches
+// for a rank: the k-th token (by count), the one at which the weights reach top_p of the sum so far (by weight), and the
+// one at which they exceed u of the kept sum (by weight).  No sort of the row: one pass counts the tokens and sums the
+// weights of 32 bins of the logit, a search opens the one bin that it ends in.
+//
+// Weights are exp of fp64 arguments, rounded once to units of 2^-47 to 2^-43 of the largest weight (by the vocabulary alone,
+// see unit_bits_of) and summed as integers.  fp32 sums of 10^5 weights would be off by some 10^-7 of their total, as much as a
+// small weight itself: the token found would depend on the order of the sum.  Integers also make results independent of
+// how many CTAs share a row.
+//
+// A row is shared by a cluster of 1 to 8 CTAs, each with a contiguous segment of it.  A thread has a column of its own in
+// the bins (32 x 512 x 8 bytes, no atomics, no bank conflicts): weight sum in the low 53 bits, count in the top 11.
+#include "ec_common.cuh"
+#include "ec_tc_ptx.cuh"
+
+#include <cooperative_groups.h>
+
+namespace ec {
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kBins = 32;                  // bin 31: weights that round to 0
+constexpr int kWeightBits = 53;            // of a thread's column of a bin; the rest counts
+constexpr int kMaxCluster = 8;
+constexpr int kSegment = kThreads * 1016;  // elements of a CTA: 1016 weights of 2^43 units fit a thread's column
+constexpr int kList = 8192;                // candidates that a search takes out of the row
+constexpr int kFew = 128;                  // candidates that are ranked against one another
+constexpr uint32_t HIST_BYTES = kBins * kThreads * 8;
+constexpr int kMaxUnitBits = 47;
+// a thread's weights, none above one, have to fit kWeightBits: as fine a unit as the whole row on one CTA leaves room for
+__host__ __device__ constexpr int unit_bits_of(int vocab) {
+    int bits = kMaxUnitBits;
+    while (bits > 43 && (long long)((vocab + 4095) / 4096 * 8) << bits > 1ll << kWeightBits) --bits;
+    return bits;
+}
+typedef unsigned long long u64;
+
+// 2^(i / 64), i = 0 .. 63, from its definition; filled once a CTA
+struct ExpTable {
+    double v[64];
+};
+
+__device__ __forceinline__ double widen(float x) {   // exact but for zero and subnormals (below 2^-126: taken as that)
+    const uint32_t b = __float_as_uint(x);
+    return __hiloint2double((int)((b & 0x80000000u) | (((b & 0x7fffffffu) >> 3) + 0x38000000u)), (int)(b << 29));
+}
+// Order of a logit as an integer, ascending with DESCENDING logits; both zeros alike
+__device__ __forceinline__ uint32_t order_of(float x) {
+    uint32_t b = __float_as_uint(x);
+    if (b == 0x80000000u) b = 0;
+    return (b & 0x80000000u) ? b : ~(b | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t o) {
+    return __uint_as_float((o & 0x80000000u) ? o : (~o & 0x7fffffffu));
+}
+
+struct Scale {   // what turns a logit of this row into a bin and a weight
+    float top, per_bin;   // bin = (top - x) * per_bin, to the nearest
+    double wide_top, c;   // (x - top) * c = 64 log2 of the weight
+    double round, unit;   // 2^(52 - bits), whose last bit is one unit of weight, and 2^bits
+};
+__device__ __forceinline__ int bin_of(const Scale& s, float x) {
+    // every step is monotone in x, so bins are intervals of the order
+    const float z = fminf((s.top - x) * s.per_bin, 31.f);
+    return __float_as_int(z + 8388608.f) & 31;
+}
+// Weight in (0, 1], relative error 1e-13: 2^(n/64) from the table, 2^(r/64) for |r| <= 1/2 by its Taylor polynomial
+// ((ln 2 / 128)^5 / 120 = 4e-14 left).  (x - top) * c must be above -64 * 60.
+struct Parts {
+    double poly, scale;
+};
+__device__ __forceinline__ Parts weight_parts(const Scale& s, const ExpTable& tab, float x) {
+    constexpr double kMagic = 6755399441055744.0;   // 1.5 * 2^52: the sum's low bits are the nearest integer
+    constexpr double a1 = 0.010830424696249145, a2 = a1 * a1 / 2, a3 = a1 * a1 * a1 / 6, a4 = a1 * a1 * a1 * a1 / 24;   // ln 2 / 64
+    const double u = (widen(x) - s.wide_top) * s.c;
+    const double km = u + kMagic;
+    const int k = __double2loint(km);
+    const double r = u - (km - kMagic);
+    const double p = fma(fma(fma(fma(a4, r, a3), r, a2), r, a1), r, 1.0);
+    const double t = tab.v[k & 63];
+    return {p, __hiloint2double(__double2hiint(t) + (k >> 6) * (1 << 20), __double2loint(t))};
+}
+__device__ __forceinline__ u64 weight_units(const Scale& s, const ExpTable& tab, float x) {
+    const Parts w = weight_parts(s, tab, x);
+    return (u64)(__double_as_longlong(fma(w.poly, w.scale, s.round)) - __double_as_longlong(s.round));
+}
+
+struct Found {    // the token that a search ends at
+    u64 count, weight;   // of the tokens up to it, itself included
+    u64 order;           // order << 32 | index
+};
+
+struct Shared {
+    ExpTable tab;
+    u64 xch[2][kMaxCluster][72];   // exchanged between the CTAs of a row: per rank 32 weights, 32 counts, 8 more
+    u64 bin_w[kBins], bin_c[kBins], all_w, all_c, red_a[kWarps], red_b[kWarps];
+    Found found;
+    u64 cand_w[kFew];
+    u64 sub_w[256];
+    uint32_t sub_c[256];
+    uint32_t n_list, n_next;
+    u64 pick[4];
+};
+
+// 8 consecutive logits, -inf past `end`
+__device__ __forceinline__ void load8(const __nv_bfloat16* row, int i, int end, float (&x)[8]) {
+    uint4 v = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
+    if (i < end) v = *reinterpret_cast<const uint4*>(row + i);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        x[2 * j] = __uint_as_float(w[j] << 16);
+        x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+    }
+    if (i + 8 > end) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (i + j >= end) x[j] = -INFINITY;
+    }
+}
+__device__ __forceinline__ void load8(const float* row, int i, int end, float (&x)[8]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        if (i + 4 * h < end) v = *reinterpret_cast<const float4*>(row + i + 4 * h);
+        x[4 * h] = v.x, x[4 * h + 1] = v.y, x[4 * h + 2] = v.z, x[4 * h + 3] = v.w;
+    }
+    if (i + 8 > end) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (i + j >= end) x[j] = -INFINITY;
+    }
+}
+
+template <typename T>
+class RowSampler {
+public:
+    __device__ RowSampler(Shared& sh, unsigned char* hist, const T* row, int begin, int end)
+        : sh(sh), hist(hist), row(row), begin(begin), end(end), cluster(cg::this_cluster()), rank(cluster.block_rank()),
+          n_ranks(cluster.num_blocks()), tid(threadIdx.x), lane(threadIdx.x & 31), warp(threadIdx.x >> 5) {}
+
+    __device__ void run(const SampleArgs& a, int r) {
+        // ---- largest logit (lowest index on ties) and the smallest finite one ----
+        u64 best = ~0ull;
+        uint32_t low = 0;
+        each([&](float x, int i) {
+            if (x > -INFINITY) {
+                const uint32_t o = order_of(x);
+                best = min(best, (u64)o << 32 | (uint32_t)i);
+                low = max(low, o);
+            }
+        });
+        u64 low64 = low;
+        block_min_max(best, low64);
+        publish(64, best), publish(65, low64);
+        const u64(*in)[72] = exchange();
+        best = ~0ull, low64 = 0;
+        for (int k = 0; k < n_ranks; ++k) best = min(best, in[k][64]), low64 = max(low64, in[k][65]);
+        const float t = a.temperature ? a.temperature[r] : 1.f;
+        if (best == ~0ull || !(t > 0.f)) {
+            if (rank == 0 && tid == 0) {
+                const bool some = best != ~0ull;
+                a.token_out[r] = some ? (int)(uint32_t)best : -1;
+                if (a.prob_out) a.prob_out[r] = some ? 1.f : 0.f;
+                if (a.kept_out) a.kept_out[r] = some ? 1 : 0;
+            }
+            return;
+        }
+        s.top = value_of((uint32_t)(best >> 32));
+        s.c = 64.0 * 1.4426950408889634074 / (double)t;
+        s.wide_top = widen(s.top);
+        const int bits = unit_bits_of(a.vocab);
+        s.round = (double)(1ull << (52 - bits)), s.unit = (double)(1ull << bits);
+        // 31 bins over the nats above half a unit, (bits + 1) ln 2 < 33.4 of them, or over the whole row where that spans less
+        const float span = (s.top - value_of((uint32_t)low64)) / t;
+        s.per_bin = fminf((span < 33.4f ? fminf(30.f / span, 1e30f) : 30.45f / 33.4f) / t, 1e37f);   // (finite: 0 times it is 0)
+        // ---- counts and weights by bin, and of the tokens that min-p keeps ----
+        const float mp = a.min_p ? a.min_p[r] : 0.f;
+        // (at least the largest stays; a bound below a unit asks the exponents instead of the weights)
+        const u64 floor_units = mp > 0.f ? (u64)fmin(ceil((double)mp * s.unit), s.unit) : 0;
+        const bool tiny = floor_units == 1;
+        const double least_u = tiny ? 64.0 * log2((double)mp) : 0.0;
+        u64* column = reinterpret_cast<u64*>(hist) + tid;
+#pragma unroll
+        for (int b = 0; b < kBins; ++b) column[b * kThreads] = 0;
+        u64 kept_c = 0, kept_w = 0;
+        each([&](float x, int) {
+            if (x == -INFINITY) return;
+            const int b = bin_of(s, x);
+            const u64 w = weight_or_0(x, b);
+            column[b * kThreads] += w + (1ull << kWeightBits);
+            if (tiny ? (widen(x) - s.wide_top) * s.c >= least_u : w >= floor_units) kept_c += 1, kept_w += w;
+        });
+        block_sum(kept_c, kept_w);
+        reduce_bins();
+        publish(64, kept_c), publish(65, kept_w);
+        const u64(*all)[72] = exchange();
+        if (tid < kBins) {
+            u64 w = 0, c = 0;
+            for (int k = 0; k < n_ranks; ++k) w += all[k][tid], c += all[k][32 + tid];
+            u64 tw = w, tc = c;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) {
+                tw += __shfl_xor_sync(0xffffffffu, tw, o);
+                tc += __shfl_xor_sync(0xffffffffu, tc, o);
+            }
+            sh.bin_w[tid] = w, sh.bin_c[tid] = c;
+            if (tid == 0) sh.all_w = tw, sh.all_c = tc;
+        }
+        kept_c = kept_w = 0;
+        for (int k = 0; k < n_ranks; ++k) kept_c += all[k][64], kept_w += all[k][65];
+        __syncthreads();
+
+        // ---- the kept prefix ----
+        u64 n = sh.all_c, sum = sh.all_w;
+        if (a.top_k) {
+            const int k = a.top_k[r];
+            if (k > 0 && (u64)k < n) {
+                const Found f = search(true, k);
+                n = k, sum = f.weight;
+            }
+        }
+        if (a.top_p) {
+            const float p = a.top_p[r];
+            if (p < 1.f) {
+                const u64 need = (u64)fmax(1.0, ceil((double)p * (double)sum));
+                const Found f = search(false, min(need, sum));
+                if (f.count < n) n = f.count, sum = f.weight;
+            }
+        }
+        if (mp > 1.f) kept_c = 1, kept_w = (u64)s.unit;   // nobody reaches it: the first token alone
+        if (floor_units && kept_c < n) n = kept_c, sum = kept_w;
+
+        // ---- the token ----
+        const u64 past = (u64)fmax(0.0, (double)a.u[r] * (double)sum) + 1;   // running sum > u * S
+        const Found f = search(false, min(past, sum));
+        if (rank == 0 && tid == 0) {
+            a.token_out[r] = (int)(uint32_t)f.order;
+            if (a.prob_out) {
+                const Parts w = weight_parts(s, sh.tab, value_of((uint32_t)(f.order >> 32)));
+                a.prob_out[r] = (float)(w.poly * w.scale * s.unit / (double)sum);
+            }
+            if (a.kept_out) a.kept_out[r] = (int)n;
+        }
+    }
+
+private:
+    Shared& sh;
+    unsigned char* hist;
+    const T* row;
+    const int begin, end;
+    cg::cluster_group cluster;
+    const int rank, n_ranks, tid, lane, warp;
+    Scale s;
+    int turn = 0;
+
+    // f(logit, index) for this CTA's segment
+    template <typename F>
+    __device__ __forceinline__ void each(F f) {
+        for (int i = begin + tid * 8; i < end; i += kThreads * 8) {
+            float x[8];
+            load8(row, i, end, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f(x[j], i + j);
+        }
+    }
+    __device__ __forceinline__ u64 weight_or_0(float x, int bin) const { return bin < 31 ? weight_units(s, sh.tab, x) : 0; }
+
+    __device__ __forceinline__ void block_min_max(u64& a, u64& b) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            a = min(a, __shfl_xor_sync(0xffffffffu, a, o));
+            b = max(b, __shfl_xor_sync(0xffffffffu, b, o));
+        }
+        __syncthreads();
+        if (lane == 0) sh.red_a[warp] = a, sh.red_b[warp] = b;
+        __syncthreads();
+        for (int k = 0; k < kWarps; ++k) a = min(a, sh.red_a[k]), b = max(b, sh.red_b[k]);
+    }
+    __device__ __forceinline__ void block_sum(u64& a, u64& b) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            a += __shfl_xor_sync(0xffffffffu, a, o);
+            b += __shfl_xor_sync(0xffffffffu, b, o);
+        }
+        __syncthreads();
+        if (lane == 0) sh.red_a[warp] = a, sh.red_b[warp] = b;
+        __syncthreads();
+        a = b = 0;
+        for (int k = 0; k < kWarps; ++k) a += sh.red_a[k], b += sh.red_b[k];
+    }
+    // the CTA's sums of the bins, to every CTA of the row
+    __device__ __forceinline__ void reduce_bins() {
+        __syncthreads();
+        const u64* h = reinterpret_cast<const u64*>(hist);
+        for (int b = warp; b < kBins; b += kWarps) {
+            u64 w = 0, c = 0;
+#pragma unroll 4
+            for (int k = lane; k < kThreads; k += 32) {
+                const u64 v = h[b * kThreads + k];
+                w += v & ((1ull << kWeightBits) - 1), c += v >> kWeightBits;
+            }
+#pragma unroll
+            for (int o = 16; o; o >>= 1) {
+                w += __shfl_xor_sync(0xffffffffu, w, o);
+                c += __shfl_xor_sync(0xffffffffu, c, o);
+            }
+            if (lane < n_ranks) {
+                u64(*to)[72] = cluster.map_shared_rank(sh.xch[turn], lane);
+                to[rank][b] = w, to[rank][32 + b] = c;
+            }
+        }
+    }
+    __device__ __forceinline__ void publish(int slot, u64 v) {
+        if (tid < n_ranks) cluster.map_shared_rank(sh.xch[turn], tid)[rank][slot] = v;
+    }
+    // what every rank has published since the last exchange; stays readable until the exchange after next
+    __device__ __forceinline__ const u64 (*exchange())[72] {
+        cluster.sync();
+        const u64(*in)[72] = sh.xch[turn];
+        turn ^= 1;
+        return in;
+    }
+
+    // The first token, in order, at which the running count (or weight) reaches `target` (1 <= target <= the total).
+    __device__ Found search(bool by_count, u64 target) {
+        // the bin
+        u64 base_c = 0, base_w = 0;
+        int bin = 0;
+        for (; bin < kBins - 1; ++bin) {
+            const u64 c = sh.bin_c[bin], w = sh.bin_w[bin];
+            if ((by_count ? base_c + c : base_w + w) >= target) break;
+            base_c += c, base_w += w;
+        }
+        if (bin == kBins - 1 && by_count) return Found{target, base_w, ~0ull};   // among the tokens of weight 0: nobody asks which
+        // [lo, hi]: the range of the order that holds it; narrowed until its tokens fit a list
+        u64 lo = 0, hi = ~0ull, in_range = sh.bin_c[bin];
+        while (in_range > kList) {
+            u64 least = ~0ull, most = 0;
+            each([&](float x, int i) {
+                const u64 o = (u64)order_of(x) << 32 | (uint32_t)i;
+                if (x > -INFINITY && bin_of(s, x) == bin && o >= lo && o <= hi) least = min(least, o), most = max(most, o);
+            });
+            block_min_max(least, most);
+            publish(64, least), publish(65, most);
+            const u64(*in)[72] = exchange();
+            least = ~0ull, most = 0;
+            for (int k = 0; k < n_ranks; ++k) least = min(least, in[k][64]), most = max(most, in[k][65]);
+            const int shift = max(0, 59 - __clzll((long long)(most - least)));   // 32 parts of the range, 16 of them used at least
+            u64* column = reinterpret_cast<u64*>(hist) + tid;
+#pragma unroll
+            for (int b = 0; b < kBins; ++b) column[b * kThreads] = 0;
+            each([&](float x, int i) {
+                const u64 o = (u64)order_of(x) << 32 | (uint32_t)i;
+                if (x > -INFINITY && bin_of(s, x) == bin && o >= lo && o <= hi)
+                    column[((o - least) >> shift) * kThreads] += weight_or_0(x, bin) + (1ull << kWeightBits);
+            });
+            reduce_bins();
+            const u64(*all)[72] = exchange();
+            int part = 0;
+            for (;; ++part) {
+                u64 c = 0, w = 0;
+                for (int k = 0; k < n_ranks; ++k) w += all[k][part], c += all[k][32 + part];
+                in_range = c;
+                if (part == kBins - 1 || (by_count ? base_c + c : base_w + w) >= target) break;
+                base_c += c, base_w += w;
+            }
+            lo = least + ((u64)part << shift);
+            hi = lo + ((1ull << shift) - 1);
+            if (hi < lo) hi = ~0ull;
+        }
+        // ---- the list: every CTA its own, then rank 0 all of them ----
+        u64* list = reinterpret_cast<u64*>(hist);
+        if (tid == 0) sh.n_list = 0;
+        __syncthreads();
+        each([&](float x, int i) {
+            const u64 o = (u64)order_of(x) << 32 | (uint32_t)i;
+            const bool in = x > -INFINITY && bin_of(s, x) == bin && o >= lo && o <= hi;
+            if (in) list[atomicAdd(&sh.n_list, 1u)] = o;
+        });
+        cluster.sync();
+        if (rank == 0) {
+            uint32_t n = sh.n_list;
+            for (int k = 1; k < n_ranks; ++k) {
+                const uint32_t more = *cluster.map_shared_rank(&sh.n_list, k);
+                const u64* from = cluster.map_shared_rank(list, k);
+                for (uint32_t i = tid; i < more; i += kThreads) list[n + i] = from[i];
+                n += more;
+            }
+            __syncthreads();
+            const Found f = select(by_count, target, base_c, base_w, list, (int)n, bin);
+            if (tid < n_ranks) *cluster.map_shared_rank(&sh.found, tid) = f;
+        }
+        cluster.sync();
+        return sh.found;
+    }
+
+    // the same over a list in shared memory, one CTA
+    __device__ Found select(bool by_count, u64 target, u64 base_c, u64 base_w, u64* list, int n, int bin) {
+        u64* other = list + kList;
+        while (n > kFew) {
+            u64 least = ~0ull, most = 0;
+            for (int i = tid; i < n; i += kThreads) least = min(least, list[i]), most = max(most, list[i]);
+            block_min_max(least, most);
+            const int shift = max(0, 56 - __clzll((long long)(most - least)));   // 256 parts
+            if (tid < 256) sh.sub_w[tid] = 0, sh.sub_c[tid] = 0;
+            if (tid == 0) sh.n_next = 0;
+            __syncthreads();
+            for (int i = tid; i < n; i += kThreads) {
+                const int part = (int)((list[i] - least) >> shift);
+                atomicAdd(&sh.sub_c[part], 1u);
+                atomicAdd(&sh.sub_w[part], weight_or_0(value_of((uint32_t)(list[i] >> 32)), bin));
+            }
+            __syncthreads();
+            if (warp == 0) {   // the part, by a scan of 8 parts a lane
+                u64 w[8], c[8], tw = 0, tc = 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[k] = sh.sub_w[lane * 8 + k], c[k] = sh.sub_c[lane * 8 + k], tw += w[k], tc += c[k];
+                u64 pw = tw, pc = tc;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const u64 xw = __shfl_up_sync(0xffffffffu, pw, o), xc = __shfl_up_sync(0xffffffffu, pc, o);
+                    if (lane >= o) pw += xw, pc += xc;
+                }
+                const bool reached = (by_count ? base_c + pc : base_w + pw) >= target;
+                const uint32_t m = __ballot_sync(0xffffffffu, reached);
+                if (lane == (m ? __ffs(m) - 1 : 31)) {
+                    u64 bw = base_w + pw - tw, bc = base_c + pc - tc;
+                    int k = 0;
+                    for (; k < 7; ++k) {
+                        if ((by_count ? bc + c[k] : bw + w[k]) >= target) break;
+                        bw += w[k], bc += c[k];
+                    }
+                    sh.pick[0] = bc, sh.pick[1] = bw, sh.pick[2] = lane * 8 + k;
+                }
+            }
+            __syncthreads();
+            base_c = sh.pick[0], base_w = sh.pick[1];
+            const int part = (int)sh.pick[2];
+            for (int i = tid; i < n; i += kThreads)
+                if ((int)((list[i] - least) >> shift) == part) other[atomicAdd(&sh.n_next, 1u)] = list[i];
+            __syncthreads();
+            n = (int)sh.n_next;
+            u64* x = list;
+            list = other, other = x;
+            __syncthreads();
+        }
+        // few: every one against every other; four threads a candidate
+        if (tid < n) sh.cand_w[tid] = weight_or_0(value_of((uint32_t)(list[tid] >> 32)), bin);
+        __syncthreads();
+        const int mine = tid >> 2;
+        u64 c = 0, w = 0;
+        const u64 me = mine < n ? list[mine] : 0;
+        if (mine < n)
+            for (int i = tid & 3; i < n; i += 4)
+                if (list[i] <= me) c += 1, w += sh.cand_w[i];
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+            c += __shfl_xor_sync(0xffffffffu, c, o);
+            w += __shfl_xor_sync(0xffffffffu, w, o);
+        }
+        if (mine < n && (tid & 3) == 0) {
+            const u64 own = sh.cand_w[mine];
+            const bool here = by_count ? base_c + c == target : base_w + w >= target && base_w + w - own < target;
+            if (here) sh.pick[0] = base_c + c, sh.pick[1] = base_w + w, sh.pick[2] = me;
+        }
+        __syncthreads();
+        const Found f{sh.pick[0], sh.pick[1], sh.pick[2]};
+        return f;
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a, int segment) {
+    extern __shared__ __align__(16) unsigned char hist[];
+    __shared__ Shared sh;
+    cg::cluster_group cluster = cg::this_cluster();
+    if (threadIdx.x < 64) sh.tab.v[threadIdx.x] = exp2((double)threadIdx.x / 64.0);
+    tc::pdl_wait();
+    tc::pdl_launch_dependents();
+    __syncthreads();
+    const int n_ranks = cluster.num_blocks(), r = blockIdx.x / n_ranks;
+    const int begin = min((int)cluster.block_rank() * segment, a.vocab), end = min(begin + segment, a.vocab);
+    RowSampler<T> row(sh, hist, static_cast<const T*>(a.logits) + r * a.row_stride, begin, end);
+    row.run(a, r);
+    cluster.sync();   // no CTA leaves while another may still write into its shared memory
+}
+
+template <typename T>
+cudaError_t launch(const SampleArgs& a, cudaStream_t stream) {
+    // CTAs of a row: all SMs at work while rows are few, and a segment that its counters can hold
+    int c = 1;
+    while (c < kMaxCluster && ((long long)a.n_rows * c * 2 <= sm_count() + 4 || a.vocab > c * (long long)kSegment) &&
+           (a.vocab > c * 4096 || a.vocab > c * (long long)kSegment))
+        c *= 2;
+    static PerDeviceOnce once;
+    if (const cudaError_t e = ensure_dynamic_smem(once, sample_kernel<T>, (int)HIST_BYTES); e != cudaSuccess) return e;
+    const int segment = ((a.vocab + c - 1) / c + 7) & ~7;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(a.n_rows * c, 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = HIST_BYTES;
+    cfg.stream = stream;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = c;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, sample_kernel<T>, a, segment);
+}
+
+}  // namespace
+
+size_t sample_workspace_bytes(int, int) { return 16; }   // everything stays in shared memory
+
+cudaError_t launch_sample(const SampleArgs& a, cudaStream_t stream) {
+    return a.dtype == EC_BF16 ? launch<__nv_bfloat16>(a, stream) : launch<float>(a, stream);
+}
+
+}  // namespace ec
