@@ -392,7 +392,9 @@ ec_status rope_call(const ec_rope_desc* desc, const void* q, int64_t q_row_strid
     return launch_rope(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? EC_OK : EC_ERR_CUDA;
 }
 
-size_t paged_ws(const ec_paged_desc& d) { return attend_paged_rows_workspace(d); }
+size_t paged_ws(const ec_paged_desc& d, int max_rows) {
+    return attend_paged_tiles_supported(d, max_rows) ? attend_paged_tiles_workspace(d) : attend_paged_rows_workspace(d);
+}
 
 ec_status check_pages(const ec_pages_desc* d, const int32_t* table, const int32_t* lens, const int32_t* refs) {
     if (!d || !table || !lens || !refs) return EC_ERR_NULL;
@@ -450,7 +452,7 @@ ec_status ec_qk_norm_rope_paged(const ec_rope_desc* desc, const ec_paged_desc* p
 
 size_t ec_attend_paged_workspace_bytes(const ec_paged_desc* desc, int32_t max_rows) {
     if (check_paged(desc) != EC_OK || max_rows < 1) return 0;
-    return paged_ws(*desc);
+    return paged_ws(*desc, max_rows);
 }
 
 ec_status ec_attend_paged(const ec_paged_desc* desc, const void* q, const int32_t* row_offsets, const int32_t* kv_lens,
@@ -465,7 +467,7 @@ ec_status ec_attend_paged(const ec_paged_desc* desc, const void* q, const int32_
     if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out) ||
         !all_aligned4(row_offsets, kv_lens, page_table, dev_status))
         return EC_ERR_ALIGN;
-    if (!workspace || workspace_bytes < paged_ws(*desc)) return EC_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < paged_ws(*desc, max_rows)) return EC_ERR_WORKSPACE;
     if (!aligned16(workspace)) return EC_ERR_ALIGN;
     PagedArgs a;
     a.d = *desc;
@@ -481,12 +483,14 @@ ec_status ec_attend_paged(const ec_paged_desc* desc, const void* q, const int32_
     a.workspace = workspace;
     a.dev_status = dev_status;
     a.scale = desc->scale > 0.f ? desc->scale : 1.0f / sqrtf((float)desc->head_dim);
-    return launch_attend_paged_rows(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? EC_OK : EC_ERR_CUDA;
+    const auto s = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = attend_paged_tiles_supported(*desc, max_rows) ? launch_attend_paged_tiles(a, s) : launch_attend_paged_rows(a, s);
+    return e == cudaSuccess ? EC_OK : EC_ERR_CUDA;
 }
 
 const char* ec_attend_paged_kernel_name(const ec_paged_desc* desc, int32_t max_rows) {
     if (check_paged(desc) != EC_OK || max_rows < 1) return "";
-    return "attend_paged_rows_kernel";
+    return attend_paged_tiles_supported(*desc, max_rows) ? "attend_paged_tiles_kernel" : "attend_paged_rows_kernel";
 }
 
 size_t ec_pages_workspace_bytes(int32_t n_pages) { return n_pages < 1 || n_pages > (1 << 28) ? 0 : pages_workspace_bytes(n_pages); }

@@ -1,0 +1,655 @@
+// ec_attend_paged for more than sixteen packed query rows a kv head (chunked prefill, blocks of mask tokens), bf16: the
+// Blackwell tensor cores, keys and values by TMA page by page.
+//
+// Bound by the tensor pipe and the exponentials where rows are many, by the K/V bytes where they are few.  One persistent
+// CTA an SM takes its stretch of the line of units (ec_paged.cuh): a unit is two tiles of 128 packed query rows of one kv head
+// over key tiles of 128.  The body is that of the dense kernel (ec_attend_dense_tc.cu, where its choices are measured):
+//   warp 0      TMA producer: a key tile is 128 / page_size pages, each one box a 64-column half (one box for both where a
+//               page is a whole tile); pages wholly behind the sequence's end are not asked for
+//   warp 1      tcgen05.mma issuer: S_t = Q_t K^T, O_t += P_t V with P in tensor memory
+//   warps 2-17  softmax, four warpgroups: (row tile) x (64-column half); no running maximum in the first pass, a row's
+//               reference is its largest score among the first eight keys of the part that it sees.  They also bring Q into
+//               shared memory (packed rows are rows of several heads and tokens: plain loads, the swizzle by hand)
+//   warp 18     zeroes the rows of the last V tile that stand behind the sequence's end (an unfinished page may hold anything,
+//               and 0 x NaN is NaN), and looks up the next unit meanwhile
+// A row sees keys below its limit; a tile whose keys are below the lowest limit of a warp's rows needs no mask.
+// Barriers are set up anew for every unit.  A unit that a cut divides leaves its un-normalised rows in the workspace, 16-byte
+// pieces swizzled by row as they stand in shared memory, for the second launch to join.
+#include "ec_paged.cuh"
+#include "ec_paged_combine.cuh"
+#include "ec_tc_ptx.cuh"
+
+namespace ec {
+namespace {
+
+using namespace tc;
+using namespace paged;
+
+constexpr int BM = 128, BN = 128;
+constexpr int kSoftThreads = 512, kThreads = 64 + kSoftThreads + 32;
+constexpr uint32_t SUB = 128 * 128;   // [128 rows x 64 bf16], 128-byte swizzle: 16 KB
+constexpr int kSlots = 5;
+struct Segment {   // what the roles know of the unit at hand
+    Unit u;
+    int j0, j1;    // key tiles of this CTA
+    int more;      // 0: nothing left
+};
+template <int HD>
+struct Geo {
+    static constexpr uint32_t TILE = HD / 64 * SUB;
+    static constexpr uint32_t OFF_Q = 0;
+    static constexpr uint32_t OFF_RING = 2 * TILE;
+    static constexpr uint32_t OFF_BAR = OFF_RING + kSlots * TILE;
+    static constexpr uint32_t OFF_SEG = OFF_BAR + 256;
+    static constexpr uint32_t OFF_XCH = OFF_SEG + 256;
+    static constexpr uint32_t NEEDED = OFF_XCH + 2 * 2 * BM * 4;
+    static constexpr uint32_t BYTES = HD == 128 ? 232448 : NEEDED + 1024;
+    static constexpr uint32_t PART = BM * HD * 4;
+    static_assert(2 * sizeof(Segment) <= 256 && NEEDED + 256 <= BYTES, "shared memory");
+    static_assert((EC_PAGED_MAX_BATCH + 1) * 8 <= kSlots * TILE && 2 * PART <= kSlots * TILE, "what stands over the ring");
+};
+constexpr uint32_t TM_COLS = 512;
+constexpr uint32_t TM_S = 0, TM_O = 256;
+
+enum { B_FULL = 0, B_FREE = kSlots, B_SFULL = B_FREE + 3, B_PFULL = B_SFULL + 2, B_PVDONE = B_PFULL + 4,
+       B_QFULL = B_PVDONE + 2, B_VERDICT = B_QFULL + 2, B_VREADY = B_VERDICT + 1, B_VZERO = B_VREADY + 1, B_COUNT = B_VZERO + 1 };
+
+constexpr float kMaxSum = 1.152921504606846976e18f;   // 2^60
+
+struct Params {
+    Plan plan;
+    const __nv_bfloat16* q;
+    __nv_bfloat16* out;
+    float* partial;
+    long long* cuts;
+    const int32_t* page_table;
+    int page_shift, n_pages, max_pages, n_q_heads;
+    float scale_log2;
+};
+
+__device__ __forceinline__ void mbar_inval(uint32_t bar) { asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+// the unit behind u on the line (there is one: the caller has steps left)
+__device__ __forceinline__ void step_unit(const Plan& p, Unit& u) {
+    u.w0 += u.steps;
+    if (++u.tile == tiles_of(p, u.s)) {
+        u.tile = 0;
+        if (++u.head == p.n_kv_heads) {
+            u.head = 0;
+            do {
+                ++u.b;
+                u.s = u.b < p.batch ? seq_of(p, u.b) : Seq{0, 1, 0};
+            } while (u.s.n == 0);
+        }
+    }
+    u.steps = steps_of(p, u.s, u.tile);
+}
+
+template <int HD>
+__global__ void __launch_bounds__(kThreads, 1)
+attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Params p) {
+    constexpr uint32_t TILE = Geo<HD>::TILE, OFF_Q = Geo<HD>::OFF_Q, OFF_RING = Geo<HD>::OFF_RING, OFF_BAR = Geo<HD>::OFF_BAR,
+                       OFF_XCH = Geo<HD>::OFF_XCH, PART = Geo<HD>::PART;
+    constexpr int CW = HD / 2, CH = CW / 8, HALVES = HD / 64;
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t base = (s2u(smem_raw) + 1023u) & ~1023u;
+    unsigned char* gbase = smem_raw + (base - s2u(smem_raw));
+    const uint32_t bars = base + OFF_BAR;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gbase + OFF_BAR + B_COUNT * 8);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(gbase + OFF_BAR + B_COUNT * 8 + 4);
+    volatile int* again = reinterpret_cast<volatile int*>(gbase + OFF_BAR + B_COUNT * 8 + 8);
+    Segment* segments = reinterpret_cast<Segment*>(gbase + Geo<HD>::OFF_SEG);   // [2]
+    float* xch = reinterpret_cast<float*>(gbase + OFF_XCH);
+    int32_t* const dev_status = p.plan.dev_status;
+    auto bar = [&](int idx) { return bars + idx * 8; };
+    if (base - s2u(smem_raw) + Geo<HD>::NEEDED > Geo<HD>::BYTES) {   // never with the 1024-byte alignment the runtime gives
+        if (threadIdx.x == 0 && dev_status) atomicExch(dev_status, (int)EC_ERR_CUDA);
+        return;
+    }
+    const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, cta = blockIdx.x;
+
+    auto set_up = [&]() {
+        for (int i = 0; i < B_COUNT; ++i)
+            mbar_init(bar(i), (i >= B_PFULL && i < B_PFULL + 4) || (i >= B_QFULL && i < B_QFULL + 2) ? 256u : 1u);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    };
+    if (tid == 0) {
+        prefetch_map(&map_k);
+        prefetch_map(&map_v);
+        set_up();
+        *abort_flag = 0;
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(s2u(tmem_slot)), "r"(TM_COLS)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        fence_before();
+    }
+    pdl_wait();
+    pdl_launch_dependents();
+    // ---- this CTA's stretch of the line (the layout stands over the ring until the first unit starts) ----
+    long long last;
+    {
+        long long* begin = reinterpret_cast<long long*>(gbase + OFF_RING);
+        lay_out(p.plan, begin);
+        const long long all = begin[p.plan.batch];
+        const int n = workers(p.plan, all, gridDim.x);
+        const long long first = cta < n ? cut_of(p.plan, begin, all, n, cta) : all;
+        last = cta < n ? cut_of(p.plan, begin, all, n, cta + 1) : all;
+        if (warp == 0) {
+            Segment s;
+            s.more = first < last;
+            if (s.more) {
+                s.u = unit_at(p.plan, begin, first);
+                s.j0 = (int)(first - s.u.w0);
+                s.j1 = (int)min((long long)s.u.steps, last - s.u.w0);
+            }
+            if (lane == 0) {
+                segments[0] = s;
+                p.cuts[cta] = first;
+                if (cta == 0) p.cuts[gridDim.x] = all;
+            }
+        }
+    }
+    fence_async_smem();   // the ring is the TMA's from here on
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    for (int at = 0; segments[at].more; at ^= 1) {
+        const Segment& seg = segments[at];
+        const int j0 = seg.j0, T = seg.j1 - j0, kv = seg.u.s.kv;
+        const int group = p.plan.group;
+        const long long r_pair = (long long)seg.u.tile * (2 * BM);
+        const int rows = (int)min((long long)seg.u.s.n * group - r_pair, (long long)(2 * BM));   // of this unit
+        const int tok0 = (int)(r_pair / group), head0 = (int)(r_pair - (long long)tok0 * group);   // of its first row
+        const int n_tiles_q = rows > BM ? 2 : 1;
+        // the tile that the sequence ends inside of, counted from j0; T or more: not here
+        const int j_end = (kv & (BN - 1)) || kv == 0 ? kv / BN - j0 : T;
+
+        if (warp == 0) {
+            // ================================ TMA producer ======================================
+            const bool elected = elect_one();
+            const int32_t* table = p.page_table + (long long)seg.u.b * p.max_pages;
+            const int ps = 1 << p.page_shift, boxes_page = ps == BN ? 1 : HALVES;
+            const int pg = lane / boxes_page, half = lane % boxes_page;   // this lane's box of a tile
+            int bad = 0;
+            auto page_of = [&](int j) -> int {
+                const int key = (j0 + j) * BN + pg * ps;
+                if (j >= T || pg * ps >= BN || key >= kv) return -1;
+                const int page = table[key >> p.page_shift];
+                if ((unsigned)page < (unsigned)p.n_pages) return page;
+                bad = 1;
+                return 0;   // (something of the pool)
+            };
+            int slot = 0, group_free = 0, page = page_of(0), page_next = page;
+            uint32_t turn = 0;
+            for (int n = 0; n < 4 * T; ++n) {   // ring entry: K_j = 2j, V_j = 2j + 1; from 2T on the second pass
+                if (n == 2 * T) {
+                    mbar_wait_warp(bar(B_VERDICT), 0, abort_flag, dev_status);
+                    if (!*again) break;
+                    page = page_of(0);
+                }
+                const int j = (n >= 2 * T ? n - 2 * T : n) >> 1;
+                if (!(n & 1)) page_next = page_of(j + 1);
+                if (n > kSlots && !(n & 1) && ++group_free == 3) group_free = 0, turn ^= 1;
+                if (n >= kSlots) mbar_wait_warp(bar(B_FREE + group_free), turn, abort_flag, dev_status);
+                const int keys = min(max(kv - (j0 + j) * BN, 0), BN), pages = (keys + ps - 1) >> p.page_shift;
+                if (elected) mbar_expect_tx(bar(B_FULL + slot), (uint32_t)(pages << p.page_shift) * (HD * 2));
+                __syncwarp();
+                if (page >= 0)
+                    tma_load_4d(base + OFF_RING + slot * TILE + half * SUB + pg * ps * 128, (n & 1) ? &map_v : &map_k, 0, 0, half,
+                                page * p.plan.n_kv_heads + seg.u.head, bar(B_FULL + slot));
+                __syncwarp();
+                if (n & 1) page = page_next;
+                if (++slot == kSlots) slot = 0;
+            }
+            if (__any_sync(0xffffffffu, bad) && elected && dev_status) atomicExch(dev_status, (int)EC_ERR_PAGE);
+            __syncwarp();
+        } else if (warp == 1) {
+            // ================================ MMA issuer ========================================
+            const bool elected = elect_one();
+            constexpr uint32_t IDESC_S = instr_desc(BN, 0), IDESC_PV = instr_desc(HD, 1);
+            const uint64_t desc_q = smem_desc(base + OFF_Q, 16, 1024);
+            auto products_s = [&](int t, uint64_t desc_k, int k0, int k1) {
+                if (elected) {
+#pragma unroll
+                    for (int k = k0; k < k1; ++k) {
+                        const uint32_t koff = ((k >> 2) * SUB + (k & 3) * 32) / 16;
+                        mma_ss(tmem + TM_S + t * 128, desc_q + t * (TILE / 16) + koff, desc_k + koff, IDESC_S, k > 0);
+                    }
+                }
+            };
+            int slot = 0, group_free = 0;
+            uint32_t phase = 0, p_phase = 0;
+            auto full = [&](int ahead) {
+                const bool wrapped = slot + ahead >= kSlots;
+                return mbar_test(bar(B_FULL + slot + ahead - (wrapped ? kSlots : 0)), phase ^ (wrapped ? 1u : 0u));
+            };
+            auto take = [&](bool landed) {
+                if (!landed) mbar_wait_warp(bar(B_FULL + slot), phase, abort_flag, dev_status);
+                const int s = slot;
+                if (++slot == kSlots) slot = 0, phase ^= 1;
+                return s;
+            };
+            auto release = [&]() {
+                if (elected) commit(bar(B_FREE + group_free));
+                if (++group_free == 3) group_free = 0;
+            };
+            constexpr int kPeek = HD / 16 - 2;
+            for (int pass = 0; pass < 2; ++pass) {
+                if (pass == 1) {
+                    mbar_wait_warp(bar(B_VERDICT), 0, abort_flag, dev_status);
+                    if (!*again) break;
+                }
+                {
+                    const uint64_t desc_k = smem_desc(base + OFF_RING + take(false) * TILE, 16, 1024);
+                    for (int t = 0; t < n_tiles_q; ++t) {
+                        mbar_wait_warp(bar(B_QFULL + t), 0, abort_flag, dev_status);
+                        fence_after();
+                        products_s(t, desc_k, 0, HD / 16);
+                        if (elected) commit(bar(B_SFULL + t));
+                    }
+                    release();
+                }
+                bool kv_ready = false, p_ready = false;
+                for (int j = 0; j < T; ++j, p_phase ^= 1) {
+                    const bool more = j + 1 < T, more2 = j + 2 < T;
+                    const uint64_t desc_v = smem_desc(base + OFF_RING + take(kv_ready) * TILE, SUB, 1024);
+                    const uint64_t desc_k = smem_desc(base + OFF_RING + (more ? take(kv_ready) : 0) * TILE, 16, 1024);
+                    if (j == j_end) {   // its V has landed: the zeroing warp's turn (which could not tell the phases of a ring slot apart)
+                        if (elected) mbar_arrive(bar(B_VREADY));
+                        mbar_wait_warp(bar(B_VZERO), pass, abort_flag, dev_status);
+                    }
+                    for (int t = 0; t < n_tiles_q; ++t) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            if (h == 1 || !p_ready) mbar_wait_warp(bar(B_PFULL + h * 2 + t), p_phase, abort_flag, dev_status);
+                            fence_after();
+                            if (elected) {
+#pragma unroll
+                                for (int i = 0; i < (h ? 2 : 6); ++i) {
+                                    const int k = h ? i * 4 + 3 : (i / 3) * 4 + i % 3;
+                                    mma_ts(tmem + TM_O + t * HD, tmem + TM_S + t * 128 + (k >> 2) * 64 + (k & 3) * 8,
+                                           desc_v + k * 128, IDESC_PV, (j > 0 || k > 0));
+                                }
+                            }
+                        }
+                        p_ready = false;
+                        if (more) {
+                            products_s(t, desc_k, 0, kPeek);
+                            const bool next_tile = t + 1 == n_tiles_q;
+                            const bool p_seen = mbar_test(bar(B_PFULL + (next_tile ? 0 : t + 1)), p_phase ^ (next_tile ? 1u : 0u));
+                            if (t == 0) kv_ready = __all_sync(0xffffffffu, full(0) && (!more2 || full(1)));
+                            p_ready = __all_sync(0xffffffffu, p_seen);
+                            products_s(t, desc_k, kPeek, HD / 16);
+                            if (elected) commit(bar(B_SFULL + t));
+                        }
+                        if (elected && (pass == 1 || !more)) commit(bar(B_PVDONE + t));
+                    }
+                    if (more) release();
+                }
+            }
+            __syncwarp();
+        } else if (warp < 2 + kSoftThreads / 32) {
+            // ================================ softmax (warps 2..17) ================================
+            const int ws = warp - 2;
+            const int t = ws >> 3, h = (ws >> 2) & 1;
+            const int quarter = warp & 3;
+            const int row = quarter * 32 + lane;
+            const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
+            const uint32_t tm_s = tmem + lane_addr + TM_S + t * 128;
+            const uint32_t tm_o = tmem + lane_addr + TM_O + t * HD;
+            float* xch_mine = xch + (t * 2 + h) * BM + row;
+            const float* xch_other = xch + (t * 2 + (1 - h)) * BM + row;
+            const int pair_bar = 1 + t * 4 + quarter;
+            unsigned char* qtile = gbase + OFF_Q + t * TILE;
+            auto piece = [&](int rw, int g) {   // 16-byte piece g of a row of the row tile: 128-byte swizzle
+                return reinterpret_cast<uint4*>(qtile + (g >> 3) * SUB + (rw >> 3) * 1024 + (rw & 7) * 128 + (((g & 7) ^ (rw & 7)) << 4));
+            };
+            // first element of packed row r of the unit (r < rows)
+            auto place = [&](int r) -> long long {
+                const unsigned pr = head0 + r, tok = pr / (unsigned)group, hh = pr - tok * group;
+                return ((long long)(seg.u.s.row0 + tok0 + (int)tok) * p.n_q_heads + seg.u.head * group + (int)hh) * HD;
+            };
+            constexpr int RW = 32 / CH;   // rows at a time, CH lanes a half row
+            const int sub = lane / CH, ch = lane % CH;
+            if (t < n_tiles_q) {
+                // ---- Q: a warp its 32 rows, its half of the columns ----
+                {
+                    uint4 x[CH];
+#pragma unroll
+                    for (int k = 0; k < CH; ++k) {
+                        const int r = t * BM + quarter * 32 + k * RW + sub;
+                        x[k] = make_uint4(0, 0, 0, 0);
+                        if (r < rows) x[k] = *reinterpret_cast<const uint4*>(p.q + place(r) + h * CW + ch * 8);
+                    }
+#pragma unroll
+                    for (int k = 0; k < CH; ++k) *piece(quarter * 32 + k * RW + sub, h * CH + ch) = x[k];
+                    fence_async_smem();
+                    mbar_arrive(bar(B_QFULL + t));
+                }
+                // keys that this row sees (rows behind the last: what the sequence has), and the fewest of the warp's
+                const int r_mine = t * BM + row;
+                const int lim = r_mine < rows ? limit_of(p.plan, seg.u.s, tok0 + (head0 + r_mine) / group) : kv;
+                const int lim_low = __reduce_min_sync(0xffffffffu, lim);
+                float m_used = 0.f, l_run = 0.f;
+                const float sl2 = p.scale_log2;
+                const f32x2 sl2_2 = pk(sl2, sl2);
+                {
+                    f32x2 mneg2 = pk(0.f, 0.f), sum2[2] = {pk(0.f, 0.f), pk(0.f, 0.f)};
+                    for (int j = 0; j < T; ++j) {
+                        mbar_wait(bar(B_SFULL + t), j & 1, abort_flag, dev_status);
+                        fence_after();
+                        if (j == 0) {
+                            uint32_t r8[8];
+                            ld8(tm_s, r8);
+                            wait_ld<8>(r8);
+                            // (a limit at or below the part's first key: the row sees nothing of the part)
+                            if (lim > j0 * BN) {
+                                float mx = __uint_as_float(r8[0]);
+#pragma unroll
+                                for (int c = 1; c < 8; ++c)
+                                    if (j0 * BN + c < lim) mx = fmaxf(mx, __uint_as_float(r8[c]));
+                                m_used = mx * sl2;
+                            }
+                            mneg2 = pk(-m_used, -m_used);
+                            named_barrier(pair_bar, 64);
+                        }
+                        uint32_t sr[2][32];
+                        ld32(tm_s + h * 64, sr[0]);
+                        wait_ld<32>(sr[0]);
+                        ld32(tm_s + h * 64 + 32, sr[1]);
+                        const int key0 = (j0 + j) * BN + h * 64;
+                        const bool masked = key0 + 64 > lim_low;
+                        const int seen = lim - key0;   // columns of this half that the row sees
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            if (q == 1) wait_ld<32>(sr[1]);
+                            if (masked) {
+#pragma unroll
+                                for (int c = 0; c < 32; ++c)
+                                    if (q * 32 + c >= seen) sr[q][c] = 0xff800000u;   // -inf
+                            }
+                            uint32_t pw[16];
+#pragma unroll
+                            for (int c = 0; c < 16; ++c) {
+                                const f32x2 d2 = fma2(pk(__uint_as_float(sr[q][2 * c]), __uint_as_float(sr[q][2 * c + 1])), sl2_2, mneg2);
+                                float d0, d1;
+                                upk(d2, d0, d1);
+                                const float e0 = fast_exp2(d0), e1 = fast_exp2(d1);
+                                sum2[c & 1] = add2(sum2[c & 1], pk(e0, e1));
+                                pw[c] = pack_bf16x2(e0, e1);
+                                if (q == 1 && c == 7) {
+                                    st8(tm_s + h * 64 + 16, pw);
+                                    wait_st();
+                                    fence_before();
+                                    mbar_arrive(bar(B_PFULL + t));
+                                }
+                            }
+                            if (q == 0) {
+                                st16(tm_s + h * 64, pw);
+                            } else {
+                                st8(tm_s + h * 64 + 24, pw + 8);
+                                wait_st();
+                                fence_before();
+                                mbar_arrive(bar(B_PFULL + 2 + t));
+                            }
+                        }
+                    }
+                    float a0, a1, b0, b1;
+                    upk(sum2[0], a0, a1);
+                    upk(sum2[1], b0, b1);
+                    l_run = (a0 + a1) + (b0 + b1);
+                }
+                const bool redo = named_barrier_or(9, n_tiles_q * 256, !(l_run <= kMaxSum));
+                if (ws == 0 && lane == 0) {
+                    *again = redo ? 1 : 0;
+                    mbar_arrive(bar(B_VERDICT));
+                }
+                // ---- second pass, only if a score left the first one's range: running maxima ----
+                if (redo) {
+                    m_used = -INFINITY;
+                    l_run = 0.f;
+                }
+                const uint32_t last_phase = redo ? T & 1 : 0;
+                for (int j = 0; redo && j < T; ++j) {
+                    mbar_wait(bar(B_SFULL + t), (T + j) & 1, abort_flag, dev_status);
+                    fence_after();
+                    uint32_t sr[BN / 2];
+                    ld32(tm_s + h * 64, sr);
+                    ld32(tm_s + h * 64 + 32, sr + 32);
+                    wait_ld<64>(sr);
+                    const int key0 = (j0 + j) * BN + h * 64;
+                    if (key0 + 64 > lim_low) {
+#pragma unroll
+                        for (int c = 0; c < 64; ++c)
+                            if (key0 + c >= lim) sr[c] = 0xff800000u;   // -inf
+                    }
+                    float mx[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) mx[c] = __uint_as_float(sr[c]);
+#pragma unroll
+                    for (int c = 4; c < 64; c += 2) mx[(c >> 1) & 3] = max3(mx[(c >> 1) & 3], __uint_as_float(sr[c]), __uint_as_float(sr[c + 1]));
+                    const float mloc = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                    *xch_mine = mloc;
+                    named_barrier(pair_bar, 64);
+                    const float m_tile = fmaxf(mloc, *xch_other) * sl2;
+                    float factor = 1.f;
+                    if (m_tile > m_used + 8.f || (m_used == -INFINITY && m_tile > -INFINITY)) {   // stale maximum allowed up to 2^8
+                        factor = (m_used == -INFINITY) ? 0.f : fast_exp2(m_used - m_tile);
+                        m_used = m_tile;
+                    }
+                    const bool need_rescale = (j > 0) && __any_sync(0xffffffffu, factor != 1.f);
+                    const float ref = m_used == -INFINITY ? 0.f : m_used;   // (a row that has seen nothing yet)
+                    const f32x2 mneg2 = pk(-ref, -ref);
+                    f32x2 sum2[2] = {pk(0.f, 0.f), pk(0.f, 0.f)};
+                    uint32_t pw[32];
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) {
+                        const f32x2 d2 = fma2(pk(__uint_as_float(sr[2 * c]), __uint_as_float(sr[2 * c + 1])), sl2_2, mneg2);
+                        float d0, d1;
+                        upk(d2, d0, d1);
+                        const float e0 = fast_exp2(d0), e1 = fast_exp2(d1);
+                        sum2[c & 1] = add2(sum2[c & 1], pk(e0, e1));
+                        pw[c] = pack_bf16x2(e0, e1);
+                    }
+                    {
+                        float a0, a1, b0, b1;
+                        upk(sum2[0], a0, a1);
+                        upk(sum2[1], b0, b1);
+                        l_run = fmaf(l_run, factor, (a0 + a1) + (b0 + b1));
+                    }
+                    if (need_rescale) {
+                        mbar_wait(bar(B_PVDONE + t), j & 1, abort_flag, dev_status);
+                        fence_after();
+#pragma unroll
+                        for (int c = 0; c < CW / 32; ++c) {
+                            uint32_t o[32];
+                            ld32(tm_o + h * CW + c * 32, o);
+                            wait_ld<32>(o);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * factor);
+                            st32(tm_o + h * CW + c * 32, o);
+                        }
+                    }
+                    st32(tm_s + h * 64, pw);
+                    wait_st();
+                    fence_before();
+                    mbar_arrive(bar(B_PFULL + t));
+                    mbar_arrive(bar(B_PFULL + 2 + t));
+                }
+
+                // ---- epilogue ------------------------------------------------------------------------
+                mbar_wait(bar(B_PVDONE + t), last_phase, abort_flag, dev_status);
+                fence_after();
+                *xch_mine = l_run;
+                named_barrier(pair_bar, 64);
+                const float l_row = l_run + *xch_other;
+                if (j0 == 0 && T == seg.u.steps) {
+                    // whole unit: normalised rows over the row tile's Q, and from there in pieces of 128 or 64 bytes to their places
+                    const float inv = l_row > 0.f ? 1.f / l_row : 0.f;
+#pragma unroll 1
+                    for (int c = 0; c < CW / 32; ++c) {
+                        uint32_t o[32];
+                        ld32(tm_o + h * CW + c * 32, o);
+                        wait_ld<32>(o);
+#pragma unroll
+                        for (int v4 = 0; v4 < 4; ++v4) {
+                            uint4 w;
+                            w.x = pack_bf16x2(__uint_as_float(o[v4 * 8 + 0]) * inv, __uint_as_float(o[v4 * 8 + 1]) * inv);
+                            w.y = pack_bf16x2(__uint_as_float(o[v4 * 8 + 2]) * inv, __uint_as_float(o[v4 * 8 + 3]) * inv);
+                            w.z = pack_bf16x2(__uint_as_float(o[v4 * 8 + 4]) * inv, __uint_as_float(o[v4 * 8 + 5]) * inv);
+                            w.w = pack_bf16x2(__uint_as_float(o[v4 * 8 + 6]) * inv, __uint_as_float(o[v4 * 8 + 7]) * inv);
+                            *piece(row, h * CH + c * 4 + v4) = w;
+                        }
+                    }
+                    __syncwarp();
+                    if (!*abort_flag) {   // a CTA whose wait gave up stores nothing
+#pragma unroll
+                        for (int k = 0; k < CH; ++k) {
+                            const int rw = quarter * 32 + k * RW + sub, r = t * BM + rw;
+                            const uint4 w = *piece(rw, h * CH + ch);
+                            if (r < rows) *reinterpret_cast<uint4*>(p.out + place(r) + h * CW + ch * 8) = w;
+                        }
+                    }
+                } else {
+                    // a part: un-normalised rows (relative to m_used), m and l; over the ring, so all products have to be through
+                    for (int tt = 0; tt < n_tiles_q; ++tt) mbar_wait(bar(B_PVDONE + tt), last_phase, abort_flag, dev_status);
+                    unsigned char* prow = gbase + OFF_RING + t * PART + row * (HD * 4);
+#pragma unroll 1
+                    for (int c = 0; c < CW / 32; ++c) {
+                        uint32_t o[32];
+                        ld32(tm_o + h * CW + c * 32, o);
+                        wait_ld<32>(o);
+#pragma unroll
+                        for (int v4 = 0; v4 < 8; ++v4)
+                            *reinterpret_cast<uint4*>(prow + (((h * (HD / 8) + c * 8 + v4) ^ (row & (HD / 4 - 1))) << 4)) =
+                                make_uint4(o[v4 * 4], o[v4 * 4 + 1], o[v4 * 4 + 2], o[v4 * 4 + 3]);
+                    }
+                    float* part = p.partial + ((long long)cta * 2 + (j0 == 0 ? 1 : 0)) * (2 * BM * (HD + 2));
+                    if (h == 0)   // (no weight on the reference of a row that saw nothing)
+                        *reinterpret_cast<float2*>(part + 2 * BM * HD + (t * BM + row) * 2) = make_float2(l_row > 0.f ? m_used : -INFINITY, l_row);
+                    fence_async_smem();
+                    named_barrier(pair_bar, 64);
+                    if (h == 0 && lane == 0 && !*abort_flag) {
+                        bulk_store(part + (t * BM + quarter * 32) * HD, base + OFF_RING + t * PART + quarter * 32 * (HD * 4), 32 * HD * 4);
+                        bulk_commit();
+                        bulk_wait();
+                    }
+                }
+            }
+            fence_before();
+        } else {
+            // ====================== the last V tile's rows behind the end; the next unit ============================
+            for (int pass = 0; pass < 2 && j_end < T; ++pass) {
+                if (pass == 1) {
+                    mbar_wait_warp(bar(B_VERDICT), 0, abort_flag, dev_status);
+                    if (!*again) break;
+                }
+                const int n = 2 * j_end + 1 + pass * 2 * T;
+                mbar_wait_warp(bar(B_VREADY), pass, abort_flag, dev_status);
+                unsigned char* v = gbase + OFF_RING + n % kSlots * TILE;
+                const int r0 = kv - (j0 + j_end) * BN;   // first row behind the end
+                for (int i = r0 * 8 + lane; i < BN * 8; i += 32)
+#pragma unroll
+                    for (int hf = 0; hf < HALVES; ++hf) *reinterpret_cast<uint4*>(v + hf * SUB + i * 16) = make_uint4(0, 0, 0, 0);
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(B_VZERO));
+            }
+            if (lane == 0) {
+                Segment s = seg;
+                s.more = s.u.w0 + s.u.steps < last;
+                if (s.more) {
+                    step_unit(p.plan, s.u);
+                    s.j0 = 0;
+                    s.j1 = (int)min((long long)s.u.steps, last - s.u.w0);
+                }
+                segments[at ^ 1] = s;
+            }
+        }
+        __syncthreads();
+        if (*abort_flag) break;   // (the same for all: read behind the barrier, written before it)
+        if (segments[at ^ 1].more) {
+            if (tid == 0) {
+                for (int i = 0; i < B_COUNT; ++i) mbar_inval(bar(i));
+                set_up();
+            }
+            __syncthreads();
+            fence_after();
+        }
+    }
+
+    __syncthreads();
+    if (warp == 1) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TM_COLS) : "memory");
+    }
+}
+
+// the pool [n_pages, n_kv_heads, page_size, HD] seen as 4-D {64 columns, position, half, page and head}
+bool make_page_map(CUtensorMap* map, const void* pool, const ec_paged_desc& d) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t row = (cuuint64_t)d.head_dim * 2, halves = (cuuint64_t)d.head_dim / 64;
+    const cuuint64_t dims[4] = {64, (cuuint64_t)d.page_size, halves, (cuuint64_t)d.n_pages * d.n_kv_heads};
+    const cuuint64_t strides[3] = {row, 128, row * d.page_size};
+    const cuuint32_t box[4] = {64, (cuuint32_t)d.page_size, d.page_size == BN ? (cuuint32_t)halves : 1, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(pool), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int HD>
+cudaError_t launch(const PagedArgs& a, cudaStream_t stream) {
+    CUtensorMap map_k, map_v;
+    if (!make_page_map(&map_k, a.k_pages, a.d) || !make_page_map(&map_v, a.v_pages, a.d)) return cudaErrorInvalidValue;
+    Params p;
+    p.plan = make_plan(a, 2 * BM, BN);
+    p.plan.min_steps = 2;
+    p.q = static_cast<const __nv_bfloat16*>(a.q);
+    p.out = static_cast<__nv_bfloat16*>(a.out);
+    p.page_table = a.page_table;
+    p.page_shift = __builtin_ctz((unsigned)a.d.page_size);
+    p.n_pages = a.d.n_pages, p.max_pages = a.d.max_pages, p.n_q_heads = a.d.n_q_heads;
+    p.scale_log2 = a.scale * kLog2e;
+    const int ctas = sm_count();
+    p.cuts = static_cast<long long*>(a.workspace);
+    p.partial = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + cuts_bytes(ctas));
+    static PerDeviceOnce once;
+    if (const cudaError_t e = ensure_dynamic_smem(once, attend_paged_tiles_kernel<HD>, (int)Geo<HD>::BYTES); e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(ctas, 1, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = Geo<HD>::BYTES;
+    cfg.stream = stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (const cudaError_t e = cudaLaunchKernelEx(&cfg, attend_paged_tiles_kernel<HD>, map_k, map_v, p); e != cudaSuccess) return e;
+    return launch_combine<__nv_bfloat16, HD, true>(p.plan, p.cuts, p.partial, a.out, a.d.n_q_heads, ctas, stream);
+}
+
+}  // namespace
+
+size_t attend_paged_tiles_workspace(const ec_paged_desc& d) {
+    const int ctas = sm_count();
+    return cuts_bytes(ctas) + (size_t)ctas * 2 * 2 * BM * (d.head_dim + 2) * 4;
+}
+bool attend_paged_tiles_supported(const ec_paged_desc& d, int max_rows) {
+    return d.dtype == EC_BF16 && (long long)max_rows * (d.n_q_heads / d.n_kv_heads) > 16 &&
+           (long long)d.n_pages * d.n_kv_heads <= 0x7fffffffll;
+}
+cudaError_t launch_attend_paged_tiles(const PagedArgs& a, cudaStream_t stream) {
+    return a.d.head_dim == 128 ? launch<128>(a, stream) : launch<64>(a, stream);
+}
+
+}  // namespace ec

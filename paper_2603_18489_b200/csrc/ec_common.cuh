@@ -196,6 +196,10 @@ struct PagedArgs {
 };
 size_t attend_paged_rows_workspace(const ec_paged_desc& d);
 cudaError_t launch_attend_paged_rows(const PagedArgs& a, cudaStream_t stream);
+// more than 16 packed rows a kv head, bf16
+bool attend_paged_tiles_supported(const ec_paged_desc& d, int max_rows);
+size_t attend_paged_tiles_workspace(const ec_paged_desc& d);
+cudaError_t launch_attend_paged_tiles(const PagedArgs& a, cudaStream_t stream);
 
 cudaError_t launch_pages_fork(const ec_pages_desc& d, int32_t* table, int32_t* lens, int32_t* refs, const int32_t* src,
                               const int32_t* dst, int n, int32_t* dev_status, cudaStream_t stream);

@@ -18,8 +18,8 @@ __device__ __forceinline__ void store4(__nv_bfloat16* dst, const float* v, float
 
 constexpr int kCombineThreads = 256;
 
-// partial: [worker][2 slots] of { rows [tm][HD], then (maximum, sum) [tm] }
-template <typename T, int HD>
+// partial: [worker][2 slots] of { rows [tm][HD], then (maximum, sum) [tm] }; kSwizzled: 16-byte piece c of row r at c ^ r
+template <typename T, int HD, bool kSwizzled>
 __global__ void __launch_bounds__(kCombineThreads) attend_paged_combine_kernel(const Plan p, const long long* cuts,
                                                                                const float* partial, T* out, int n_q_heads,
                                                                                int ctas) {
@@ -61,7 +61,10 @@ __global__ void __launch_bounds__(kCombineThreads) attend_paged_combine_kernel(c
 #pragma unroll 4
             for (int i = 0; i < here; ++i) {
                 const float g = __shfl_sync(0xffffffffu, f, i);
-                const float* src = part_at(i0 + i) + r * HD + lane * (HD / 32);
+                constexpr int PIECES = HD / 4;
+                int at = lane * (HD / 32);
+                if constexpr (kSwizzled) at = (((at >> 2) ^ ((int)r & (PIECES - 1))) << 2) | (at & 3);
+                const float* src = part_at(i0 + i) + r * HD + at;
                 if constexpr (HD == 128) {
                     const float4 x = *reinterpret_cast<const float4*>(src);
                     acc[0] = fmaf(g, x.x, acc[0]), acc[1] = fmaf(g, x.y, acc[1]);
@@ -108,7 +111,7 @@ inline Plan make_plan(const PagedArgs& a, int tm, int tk) {
     return p;
 }
 
-template <typename T, int HD>
+template <typename T, int HD, bool kSwizzled = false>
 cudaError_t launch_combine(const Plan& p, const long long* cuts, const float* partial, void* out, int n_q_heads, int ctas,
                            cudaStream_t stream) {
     if (ctas < 2) return cudaSuccess;
@@ -121,7 +124,7 @@ cudaError_t launch_combine(const Plan& p, const long long* cuts, const float* pa
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attend_paged_combine_kernel<T, HD>, p, cuts, partial, static_cast<T*>(out), n_q_heads, ctas);
+    return cudaLaunchKernelEx(&cfg, attend_paged_combine_kernel<T, HD, kSwizzled>, p, cuts, partial, static_cast<T*>(out), n_q_heads, ctas);
 }
 
 }  // namespace paged
