@@ -37,7 +37,7 @@ struct Params {
     const void *q, *k, *v;
     void* out;
     float* partial;
-    long long* cuts;
+    Cut* cuts;
     const int32_t* page_table;
     int page_shift, n_pages, max_pages, n_q_heads;
     float scale_log2;
@@ -286,10 +286,10 @@ __global__ void __launch_bounds__(kThreads, Geo<T, HD>::CTAS) attend_paged_rows_
     lay_out(p.plan, begin);
     const long long all = begin[p.plan.batch];
     const int n = workers(p.plan, all, gridDim.x), cta = blockIdx.x;
-    const long long first = cta < n ? cut_of(p.plan, begin, all, n, cta) : all;
-    const long long last = cta < n ? cut_of(p.plan, begin, all, n, cta + 1) : all;
-    if (threadIdx.x == 0) p.cuts[cta] = first;
-    if (threadIdx.x == 0 && cta == 0) p.cuts[gridDim.x] = all;
+    const Cut cut = cut_of(p.plan, begin, all, n, cta);
+    const long long first = cut.w, last = cut_of(p.plan, begin, all, n, cta + 1).w;
+    if (threadIdx.x == 0) p.cuts[cta] = cut;
+    if (threadIdx.x == 0 && cta == 0) p.cuts[gridDim.x] = cut_of_end(all);
 
     for (long long w = first; w < last;) {
         const Unit u = unit_at(p.plan, begin, w);
@@ -404,7 +404,7 @@ cudaError_t launch(const PagedArgs& a, cudaStream_t stream) {
     p.n_pages = a.d.n_pages, p.max_pages = a.d.max_pages, p.n_q_heads = a.d.n_q_heads;
     p.scale_log2 = a.scale * kLog2e;
     const int ctas = sm_count() * G::CTAS;
-    p.cuts = static_cast<long long*>(a.workspace);
+    p.cuts = static_cast<Cut*>(a.workspace);
     p.partial = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + cuts_bytes(ctas));
     static PerDeviceOnce once;
     if (const cudaError_t e = ensure_dynamic_smem(once, attend_paged_rows_kernel<T, HD>, G::BYTES); e != cudaSuccess) return e;

@@ -61,7 +61,7 @@ struct Params {
     const __nv_bfloat16* q;
     __nv_bfloat16* out;
     float* partial;
-    long long* cuts;
+    Cut* cuts;
     const int32_t* page_table;
     int page_shift, n_pages, max_pages, n_q_heads;
     float scale_log2;
@@ -138,8 +138,9 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
         lay_out(p.plan, begin);
         const long long all = begin[p.plan.batch];
         const int n = workers(p.plan, all, gridDim.x);
-        const long long first = cta < n ? cut_of(p.plan, begin, all, n, cta) : all;
-        last = cta < n ? cut_of(p.plan, begin, all, n, cta + 1) : all;
+        const Cut cut = cut_of(p.plan, begin, all, n, cta);
+        const long long first = cut.w;
+        last = cut_of(p.plan, begin, all, n, cta + 1).w;
         if (warp == 0) {
             Segment s;
             s.more = first < last;
@@ -150,8 +151,8 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
             }
             if (lane == 0) {
                 segments[0] = s;
-                p.cuts[cta] = first;
-                if (cta == 0) p.cuts[gridDim.x] = all;
+                p.cuts[cta] = cut;
+                if (cta == 0) p.cuts[gridDim.x] = cut_of_end(all);
             }
         }
     }
@@ -168,6 +169,10 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
         const int rows = (int)min((long long)seg.u.s.n * group - r_pair, (long long)(2 * BM));   // of this unit
         const int tok0 = (int)(r_pair / group), head0 = (int)(r_pair - (long long)tok0 * group);   // of its first row
         const int n_tiles_q = rows > BM ? 2 : 1;
+        // One row tile: the two halves of the CTA take its even and its odd key tiles, each with a reference and an accumulator of
+        // its own, so that the softmax of one tile runs under the products of the other; the rows are joined at the end.
+        const bool split = n_tiles_q == 1 && T > 1;
+        const int n_chains = split ? 2 : n_tiles_q;
         // the tile that the sequence ends inside of, counted from j0; T or more: not here
         const int j_end = (kv & (BN - 1)) || kv == 0 ? kv / BN - j0 : T;
 
@@ -186,26 +191,43 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                 bad = 1;
                 return 0;   // (something of the pool)
             };
-            int slot = 0, group_free = 0, page = page_of(0), page_next = page;
+            // Ring entries, from 2T on those of the second pass: K_0 V_0 K_1 V_1 ..., with split K_0 K_1 V_0 K_2 V_1 ... V_T-2 V_T-1.
+            // A K tile's pages are looked up one K tile ahead; those of the V tiles to come are kept: one, with split
+            // that of the tile before too.
+            int slot = 0, group_free = 0, ahead = page_of(0), kept = -1, kept_next = -1;
             uint32_t turn = 0;
-            for (int n = 0; n < 4 * T; ++n) {   // ring entry: K_j = 2j, V_j = 2j + 1; from 2T on the second pass
+            for (int n = 0; n < 4 * T; ++n) {
                 if (n == 2 * T) {
                     mbar_wait_warp(bar(B_VERDICT), 0, abort_flag, dev_status);
                     if (!*again) break;
-                    page = page_of(0);
+                    ahead = page_of(0);
                 }
-                const int j = (n >= 2 * T ? n - 2 * T : n) >> 1;
-                if (!(n & 1)) page_next = page_of(j + 1);
+                const int m = n >= 2 * T ? n - 2 * T : n;
+                bool is_v = m & 1;
+                int j = m >> 1;
+                if (split && m > 0) {
+                    is_v = !(m & 1) || m == 2 * T - 1;
+                    j = m == 2 * T - 1 ? T - 1 : is_v ? (m - 2) >> 1 : (m + 1) >> 1;
+                }
+                int page;
+                if (is_v) {
+                    page = kept;
+                    kept = kept_next;
+                } else {
+                    page = ahead;
+                    if (split && j > 0) kept_next = page;   // (V_j-1 is still to come)
+                    else kept = page;
+                    ahead = page_of(j + 1);
+                }
                 if (n > kSlots && !(n & 1) && ++group_free == 3) group_free = 0, turn ^= 1;
                 if (n >= kSlots) mbar_wait_warp(bar(B_FREE + group_free), turn, abort_flag, dev_status);
                 const int keys = min(max(kv - (j0 + j) * BN, 0), BN), pages = (keys + ps - 1) >> p.page_shift;
                 if (elected) mbar_expect_tx(bar(B_FULL + slot), (uint32_t)(pages << p.page_shift) * (HD * 2));
                 __syncwarp();
                 if (page >= 0)
-                    tma_load_4d(base + OFF_RING + slot * TILE + half * SUB + pg * ps * 128, (n & 1) ? &map_v : &map_k, 0, 0, half,
+                    tma_load_4d(base + OFF_RING + slot * TILE + half * SUB + pg * ps * 128, is_v ? &map_v : &map_k, 0, 0, half,
                                 page * p.plan.n_kv_heads + seg.u.head, bar(B_FULL + slot));
                 __syncwarp();
-                if (n & 1) page = page_next;
                 if (++slot == kSlots) slot = 0;
             }
             if (__any_sync(0xffffffffu, bad) && elected && dev_status) atomicExch(dev_status, (int)EC_ERR_PAGE);
@@ -215,14 +237,32 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
             const bool elected = elect_one();
             constexpr uint32_t IDESC_S = instr_desc(BN, 0), IDESC_PV = instr_desc(HD, 1);
             const uint64_t desc_q = smem_desc(base + OFF_Q, 16, 1024);
-            auto products_s = [&](int t, uint64_t desc_k, int k0, int k1) {
+            auto scores = [&](int t, uint64_t desc_rows, uint64_t desc_k, int k0, int k1) {
                 if (elected) {
 #pragma unroll
                     for (int k = k0; k < k1; ++k) {
                         const uint32_t koff = ((k >> 2) * SUB + (k & 3) * 32) / 16;
-                        mma_ss(tmem + TM_S + t * 128, desc_q + t * (TILE / 16) + koff, desc_k + koff, IDESC_S, k > 0);
+                        mma_ss(tmem + TM_S + t * 128, desc_rows + koff, desc_k + koff, IDESC_S, k > 0);
                     }
                 }
+            };
+            auto products_s = [&](int t, uint64_t desc_k, int k0, int k1) { scores(t, desc_q + t * (TILE / 16), desc_k, k0, k1); };
+            // P V of part h of the probabilities: the first 48 keys of each half of the tile, then the others
+            auto outputs = [&](int t, uint64_t desc_v, int h, bool add) {
+                if (elected) {
+#pragma unroll
+                    for (int i = 0; i < 6; ++i) {
+                        if (h && i >= 2) break;
+                        const int k = h ? i * 4 + 3 : (i / 3) * 4 + i % 3;
+                        mma_ts(tmem + TM_O + t * HD, tmem + TM_S + t * 128 + (k >> 2) * 64 + (k & 3) * 8, desc_v + k * 128, IDESC_PV,
+                               add || k > 0);
+                    }
+                }
+            };
+            // a V tile that the sequence ends in has landed: the zeroing warp's turn (it could not tell the phases of a ring slot apart)
+            auto zeroed = [&](int pass) {
+                if (elected) mbar_arrive(bar(B_VREADY));
+                mbar_wait_warp(bar(B_VZERO), pass, abort_flag, dev_status);
             };
             int slot = 0, group_free = 0;
             uint32_t phase = 0, p_phase = 0;
@@ -246,6 +286,35 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                     mbar_wait_warp(bar(B_VERDICT), 0, abort_flag, dev_status);
                     if (!*again) break;
                 }
+                if (split) {
+                    for (int t = 0; t < 2; ++t) {   // both chains have Q_0
+                        const uint64_t desc_k = smem_desc(base + OFF_RING + take(false) * TILE, 16, 1024);
+                        mbar_wait_warp(bar(B_QFULL), 0, abort_flag, dev_status);
+                        fence_after();
+                        scores(t, desc_q, desc_k, 0, HD / 16);
+                        if (elected) commit(bar(B_SFULL + t));
+                        if (t == 0) release();
+                    }
+                    for (int j = 0; j < T; ++j) {
+                        const int t = j & 1;
+                        const uint64_t desc_v = smem_desc(base + OFF_RING + take(false) * TILE, SUB, 1024);
+                        if (j == j_end) zeroed(pass);
+                        for (int h = 0; h < 2; ++h) {
+                            mbar_wait_warp(bar(B_PFULL + h * 2 + t), (p_phase >> t) & 1, abort_flag, dev_status);
+                            fence_after();
+                            outputs(t, desc_v, h, j > 1);
+                        }
+                        p_phase ^= 1u << t;
+                        if (j + 1 < T) release();   // V_j and K_j+1
+                        if (j + 2 < T) {
+                            const uint64_t desc_k = smem_desc(base + OFF_RING + take(false) * TILE, 16, 1024);
+                            scores(t, desc_q, desc_k, 0, HD / 16);
+                            if (elected) commit(bar(B_SFULL + t));
+                        }
+                        if (elected && (pass == 1 || j + 2 >= T)) commit(bar(B_PVDONE + t));
+                    }
+                    continue;
+                }
                 {
                     const uint64_t desc_k = smem_desc(base + OFF_RING + take(false) * TILE, 16, 1024);
                     for (int t = 0; t < n_tiles_q; ++t) {
@@ -261,23 +330,13 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                     const bool more = j + 1 < T, more2 = j + 2 < T;
                     const uint64_t desc_v = smem_desc(base + OFF_RING + take(kv_ready) * TILE, SUB, 1024);
                     const uint64_t desc_k = smem_desc(base + OFF_RING + (more ? take(kv_ready) : 0) * TILE, 16, 1024);
-                    if (j == j_end) {   // its V has landed: the zeroing warp's turn (which could not tell the phases of a ring slot apart)
-                        if (elected) mbar_arrive(bar(B_VREADY));
-                        mbar_wait_warp(bar(B_VZERO), pass, abort_flag, dev_status);
-                    }
+                    if (j == j_end) zeroed(pass);
                     for (int t = 0; t < n_tiles_q; ++t) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             if (h == 1 || !p_ready) mbar_wait_warp(bar(B_PFULL + h * 2 + t), p_phase, abort_flag, dev_status);
                             fence_after();
-                            if (elected) {
-#pragma unroll
-                                for (int i = 0; i < (h ? 2 : 6); ++i) {
-                                    const int k = h ? i * 4 + 3 : (i / 3) * 4 + i % 3;
-                                    mma_ts(tmem + TM_O + t * HD, tmem + TM_S + t * 128 + (k >> 2) * 64 + (k & 3) * 8,
-                                           desc_v + k * 128, IDESC_PV, (j > 0 || k > 0));
-                                }
-                            }
+                            outputs(t, desc_v, h, j > 0);
                         }
                         p_ready = false;
                         if (more) {
@@ -318,9 +377,12 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
             };
             constexpr int RW = 32 / CH;   // rows at a time, CH lanes a half row
             const int sub = lane / CH, ch = lane % CH;
-            if (t < n_tiles_q) {
+            if (t < n_chains) {
+                const int tq = split ? 0 : t;              // row tile
+                const int js = split ? 2 : 1;              // key tiles jt, jt + js, ...: nt of them
+                const int jt = split ? t : 0, nt = (T - jt + js - 1) / js;
                 // ---- Q: a warp its 32 rows, its half of the columns ----
-                {
+                if (tq == t) {
                     uint4 x[CH];
 #pragma unroll
                     for (int k = 0; k < CH; ++k) {
@@ -334,7 +396,7 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                     mbar_arrive(bar(B_QFULL + t));
                 }
                 // keys that this row sees (rows behind the last: what the sequence has), and the fewest of the warp's
-                const int r_mine = t * BM + row;
+                const int r_mine = tq * BM + row;
                 const int lim = r_mine < rows ? limit_of(p.plan, seg.u.s, tok0 + (head0 + r_mine) / group) : kv;
                 const int lim_low = __reduce_min_sync(0xffffffffu, lim);
                 float m_used = 0.f, l_run = 0.f;
@@ -342,19 +404,20 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                 const f32x2 sl2_2 = pk(sl2, sl2);
                 {
                     f32x2 mneg2 = pk(0.f, 0.f), sum2[2] = {pk(0.f, 0.f), pk(0.f, 0.f)};
-                    for (int j = 0; j < T; ++j) {
-                        mbar_wait(bar(B_SFULL + t), j & 1, abort_flag, dev_status);
+                    int key0 = (j0 + jt) * BN;   // of the tile
+                    for (int i = 0; i < nt; ++i, key0 += js * BN) {
+                        mbar_wait(bar(B_SFULL + t), i & 1, abort_flag, dev_status);
                         fence_after();
-                        if (j == 0) {
+                        if (i == 0) {
                             uint32_t r8[8];
                             ld8(tm_s, r8);
                             wait_ld<8>(r8);
-                            // (a limit at or below the part's first key: the row sees nothing of the part)
-                            if (lim > j0 * BN) {
+                            // (a limit at or below the first key: the row sees nothing of this part)
+                            if (lim > key0) {
                                 float mx = __uint_as_float(r8[0]);
 #pragma unroll
                                 for (int c = 1; c < 8; ++c)
-                                    if (j0 * BN + c < lim) mx = fmaxf(mx, __uint_as_float(r8[c]));
+                                    if (key0 + c < lim) mx = fmaxf(mx, __uint_as_float(r8[c]));
                                 m_used = mx * sl2;
                             }
                             mneg2 = pk(-m_used, -m_used);
@@ -364,9 +427,8 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                         ld32(tm_s + h * 64, sr[0]);
                         wait_ld<32>(sr[0]);
                         ld32(tm_s + h * 64 + 32, sr[1]);
-                        const int key0 = (j0 + j) * BN + h * 64;
-                        const bool masked = key0 + 64 > lim_low;
-                        const int seen = lim - key0;   // columns of this half that the row sees
+                        const bool masked = key0 + h * 64 + 64 > lim_low;
+                        const int seen = lim - key0 - h * 64;   // columns of this half that the row sees
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
                             if (q == 1) wait_ld<32>(sr[1]);
@@ -406,7 +468,7 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                     upk(sum2[1], b0, b1);
                     l_run = (a0 + a1) + (b0 + b1);
                 }
-                const bool redo = named_barrier_or(9, n_tiles_q * 256, !(l_run <= kMaxSum));
+                const bool redo = named_barrier_or(9, n_chains * 256, !(l_run <= kMaxSum));
                 if (ws == 0 && lane == 0) {
                     *again = redo ? 1 : 0;
                     mbar_arrive(bar(B_VERDICT));
@@ -416,15 +478,15 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                     m_used = -INFINITY;
                     l_run = 0.f;
                 }
-                const uint32_t last_phase = redo ? T & 1 : 0;
-                for (int j = 0; redo && j < T; ++j) {
-                    mbar_wait(bar(B_SFULL + t), (T + j) & 1, abort_flag, dev_status);
+                const uint32_t last_phase = redo ? nt & 1 : 0;
+                for (int i = 0; redo && i < nt; ++i) {
+                    mbar_wait(bar(B_SFULL + t), (nt + i) & 1, abort_flag, dev_status);
                     fence_after();
                     uint32_t sr[BN / 2];
                     ld32(tm_s + h * 64, sr);
                     ld32(tm_s + h * 64 + 32, sr + 32);
                     wait_ld<64>(sr);
-                    const int key0 = (j0 + j) * BN + h * 64;
+                    const int key0 = (j0 + jt + i * js) * BN + h * 64;
                     if (key0 + 64 > lim_low) {
 #pragma unroll
                         for (int c = 0; c < 64; ++c)
@@ -444,7 +506,7 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                         factor = (m_used == -INFINITY) ? 0.f : fast_exp2(m_used - m_tile);
                         m_used = m_tile;
                     }
-                    const bool need_rescale = (j > 0) && __any_sync(0xffffffffu, factor != 1.f);
+                    const bool need_rescale = (i > 0) && __any_sync(0xffffffffu, factor != 1.f);
                     const float ref = m_used == -INFINITY ? 0.f : m_used;   // (a row that has seen nothing yet)
                     const f32x2 mneg2 = pk(-ref, -ref);
                     f32x2 sum2[2] = {pk(0.f, 0.f), pk(0.f, 0.f)};
@@ -465,7 +527,7 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                         l_run = fmaf(l_run, factor, (a0 + a1) + (b0 + b1));
                     }
                     if (need_rescale) {
-                        mbar_wait(bar(B_PVDONE + t), j & 1, abort_flag, dev_status);
+                        mbar_wait(bar(B_PVDONE + t), i & 1, abort_flag, dev_status);
                         fence_after();
 #pragma unroll
                         for (int c = 0; c < CW / 32; ++c) {
@@ -473,7 +535,7 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                             ld32(tm_o + h * CW + c * 32, o);
                             wait_ld<32>(o);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * factor);
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
                             st32(tm_o + h * CW + c * 32, o);
                         }
                     }
@@ -489,15 +551,47 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                 fence_after();
                 *xch_mine = l_run;
                 named_barrier(pair_bar, 64);
-                const float l_row = l_run + *xch_other;
-                if (j0 == 0 && T == seg.u.steps) {
+                float l_row = l_run + *xch_other;
+                float own = 1.f, odd = 0.f;   // weights of this chain's accumulator and, with split, of the odd tiles'
+                if (split) {
+                    named_barrier(pair_bar, 64);   // the halves' sums have been read
+                    if (l_row == 0.f) m_used = -INFINITY;
+                    if (h == 0) xch[t * 2 * BM + row] = m_used, xch[(t * 2 + 1) * BM + row] = l_row;   // (each chain in its own)
+                    fence_before();
+                    named_barrier(10, 512);        // (and every product is through, see the wait above)
+                    fence_after();
+                    const float m_odd = xch[2 * BM + row], l_odd = xch[3 * BM + row];
+                    if (t == 0) {
+                        const float M = fmaxf(m_used, m_odd), ref = M == -INFINITY ? 0.f : M;
+                        own = fast_exp2(m_used - ref), odd = fast_exp2(m_odd - ref);
+                        l_row = fmaf(own, l_row, odd * l_odd);
+                        m_used = M;
+                    }
+                }
+                // 32 columns of the row's output, un-normalised
+                auto columns = [&](int c, uint32_t(&o)[32]) {
+                    ld32(tm_o + h * CW + c * 32, o);
+                    wait_ld<32>(o);
+                    if (split) {
+#pragma unroll
+                        for (int part = 0; part < 2; ++part) {
+                            uint32_t x[16];
+                            ld16(tm_o + HD + h * CW + c * 32 + part * 16, x);
+                            wait_ld<16>(x);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                o[part * 16 + e] = __float_as_uint(fmaf(own, __uint_as_float(o[part * 16 + e]), odd * __uint_as_float(x[e])));
+                        }
+                    }
+                };
+                const bool writes = tq == t;
+                if (writes && j0 == 0 && T == seg.u.steps) {
                     // whole unit: normalised rows over the row tile's Q, and from there in pieces of 128 or 64 bytes to their places
                     const float inv = l_row > 0.f ? 1.f / l_row : 0.f;
 #pragma unroll 1
                     for (int c = 0; c < CW / 32; ++c) {
                         uint32_t o[32];
-                        ld32(tm_o + h * CW + c * 32, o);
-                        wait_ld<32>(o);
+                        columns(c, o);
 #pragma unroll
                         for (int v4 = 0; v4 < 4; ++v4) {
                             uint4 w;
@@ -517,29 +611,32 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                             if (r < rows) *reinterpret_cast<uint4*>(p.out + place(r) + h * CW + ch * 8) = w;
                         }
                     }
-                } else {
+                } else if (writes) {
                     // a part: un-normalised rows (relative to m_used), m and l; over the ring, so all products have to be through
-                    for (int tt = 0; tt < n_tiles_q; ++tt) mbar_wait(bar(B_PVDONE + tt), last_phase, abort_flag, dev_status);
-                    unsigned char* prow = gbase + OFF_RING + t * PART + row * (HD * 4);
-#pragma unroll 1
-                    for (int c = 0; c < CW / 32; ++c) {
-                        uint32_t o[32];
-                        ld32(tm_o + h * CW + c * 32, o);
-                        wait_ld<32>(o);
-#pragma unroll
-                        for (int v4 = 0; v4 < 8; ++v4)
-                            *reinterpret_cast<uint4*>(prow + (((h * (HD / 8) + c * 8 + v4) ^ (row & (HD / 4 - 1))) << 4)) =
-                                make_uint4(o[v4 * 4], o[v4 * 4 + 1], o[v4 * 4 + 2], o[v4 * 4 + 3]);
-                    }
+                    if (!split)
+                        for (int tt = 0; tt < n_tiles_q; ++tt) mbar_wait(bar(B_PVDONE + tt), last_phase, abort_flag, dev_status);
                     float* part = p.partial + ((long long)cta * 2 + (j0 == 0 ? 1 : 0)) * (2 * BM * (HD + 2));
-                    if (h == 0)   // (no weight on the reference of a row that saw nothing)
-                        *reinterpret_cast<float2*>(part + 2 * BM * HD + (t * BM + row) * 2) = make_float2(l_row > 0.f ? m_used : -INFINITY, l_row);
-                    fence_async_smem();
-                    named_barrier(pair_bar, 64);
-                    if (h == 0 && lane == 0 && !*abort_flag) {
-                        bulk_store(part + (t * BM + quarter * 32) * HD, base + OFF_RING + t * PART + quarter * 32 * (HD * 4), 32 * HD * 4);
-                        bulk_commit();
-                        bulk_wait();
+                    const bool any = t * BM + quarter * 32 < rows;   // of this warp's rows
+                    if (any) {
+                        unsigned char* prow = gbase + OFF_RING + t * PART + row * (HD * 4);
+#pragma unroll 1
+                        for (int c = 0; c < CW / 32; ++c) {
+                            uint32_t o[32];
+                            columns(c, o);
+#pragma unroll
+                            for (int v4 = 0; v4 < 8; ++v4)
+                                *reinterpret_cast<uint4*>(prow + (((h * (HD / 8) + c * 8 + v4) ^ (row & (HD / 4 - 1))) << 4)) =
+                                    make_uint4(o[v4 * 4], o[v4 * 4 + 1], o[v4 * 4 + 2], o[v4 * 4 + 3]);
+                        }
+                        if (h == 0)   // (no weight on the reference of a row that saw nothing)
+                            *reinterpret_cast<float2*>(part + 2 * BM * HD + (t * BM + row) * 2) = make_float2(l_row > 0.f ? m_used : -INFINITY, l_row);
+                        fence_async_smem();
+                        named_barrier(pair_bar, 64);
+                        if (h == 0 && lane == 0 && !*abort_flag) {
+                            bulk_store(part + (t * BM + quarter * 32) * HD, base + OFF_RING + t * PART + quarter * 32 * (HD * 4), 32 * HD * 4);
+                            bulk_commit();
+                            bulk_wait();
+                        }
                     }
                 }
             }
@@ -551,7 +648,7 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                     mbar_wait_warp(bar(B_VERDICT), 0, abort_flag, dev_status);
                     if (!*again) break;
                 }
-                const int n = 2 * j_end + 1 + pass * 2 * T;
+                const int n = 2 * j_end + (split && j_end < T - 1 ? 2 : 1) + pass * 2 * T;   // its ring entry
                 mbar_wait_warp(bar(B_VREADY), pass, abort_flag, dev_status);
                 unsigned char* v = gbase + OFF_RING + n % kSlots * TILE;
                 const int r0 = kv - (j0 + j_end) * BN;   // first row behind the end
@@ -620,7 +717,7 @@ cudaError_t launch(const PagedArgs& a, cudaStream_t stream) {
     p.n_pages = a.d.n_pages, p.max_pages = a.d.max_pages, p.n_q_heads = a.d.n_q_heads;
     p.scale_log2 = a.scale * kLog2e;
     const int ctas = sm_count();
-    p.cuts = static_cast<long long*>(a.workspace);
+    p.cuts = static_cast<Cut*>(a.workspace);
     p.partial = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + cuts_bytes(ctas));
     static PerDeviceOnce once;
     if (const cudaError_t e = ensure_dynamic_smem(once, attend_paged_tiles_kernel<HD>, (int)Geo<HD>::BYTES); e != cudaSuccess) return e;

@@ -147,19 +147,27 @@ __device__ __forceinline__ int workers(const Plan& p, long long all, int ctas) {
     const long long n = (all + p.min_steps - 1) / p.min_steps;
     return (int)min((long long)ctas, max(n, 1ll));
 }
-// first step of CTA c of `n`.  A cut that would leave a quarter of its unit or less on one side is moved to that end of the unit
+// Start of a CTA's stretch, and the unit that it falls into
+struct Cut {
+    long long w;    // first step, all steps where there is nothing left
+    long long w0;   // first step of the unit (w0 < w: the cut divides it), -1 where there is nothing left
+    int steps, head, tile, row0, n, pad;
+};
+__device__ __forceinline__ Cut cut_of_end(long long all) { return Cut{all, -1, 0, 0, 0, 0, 0, 0}; }
+// The cut before CTA c of `n`.  One that would leave a quarter of its unit or less on one side is moved to that end of the unit
 // where the steps allow it (the partial rows of a unit cost about as much as a step).
-__device__ __forceinline__ long long cut_of(const Plan& p, const long long* begin, long long all, int n, int c) {
-    if (c <= 0) return 0;
-    if (c >= n) return all;
-    const long long w = all / n * c + all % n * c / n;
+__device__ __forceinline__ Cut cut_of(const Plan& p, const long long* begin, long long all, int n, int c) {
+    if (c >= n || all == 0) return cut_of_end(all);
+    long long w = c <= 0 ? 0 : all / n * c + all % n * c / n;
     const Unit u = unit_at(p, begin, w);
     const int in = (int)(w - u.w0);
-    if (in == 0) return w;
-    const int slack = u.steps / 4 < p.min_steps / 2 ? u.steps / 4 : p.min_steps / 2;
-    if (in <= slack) return u.w0;
-    if (u.steps - in <= slack) return u.w0 + u.steps;
-    return w;
+    if (in > 0) {
+        const int slack = u.steps / 4 < p.min_steps / 2 ? u.steps / 4 : p.min_steps / 2;
+        if (in <= slack) w = u.w0;
+        else if (u.steps - in <= slack) w = u.w0 + u.steps;
+    }
+    const bool inside = w < u.w0 + u.steps;   // (at the end of a unit nothing is divided)
+    return Cut{w, inside ? u.w0 : w, u.steps, u.head, u.tile, u.s.row0, u.s.n, 0};
 }
 
 }  // namespace paged

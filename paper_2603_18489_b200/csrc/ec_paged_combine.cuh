@@ -1,6 +1,6 @@
 // Joins the partial rows of the units that a cut divided (see ec_paged.cuh): the second launch of ec_attend_paged.
 // CTA c looks after the cut at the start of worker c.  Where it divides a unit into P parts, the P - 1 CTAs of its cuts
-// share the unit's rows; a warp takes a row: weights 2^(m_i - M) / sum, then the rows, four columns a lane.
+// share the unit's rows: weights 2^(m_i - M) / sum first, then the rows.
 #pragma once
 
 #include "ec_paged.cuh"
@@ -16,81 +16,106 @@ __device__ __forceinline__ void store4(__nv_bfloat16* dst, const float* v, float
     *reinterpret_cast<uint2*>(dst) = make_uint2(tc::pack_bf16x2(v[0] * f, v[1] * f), tc::pack_bf16x2(v[2] * f, v[3] * f));
 }
 
-constexpr int kCombineThreads = 256;
+constexpr int kCombineThreads = 512;
+constexpr int kMaxWeights = 2048;   // 2 x 256, and 256 + 2 x the parts (at most one a CTA)
 
 // partial: [worker][2 slots] of { rows [tm][HD], then (maximum, sum) [tm] }; kSwizzled: 16-byte piece c of row r at c ^ r
 template <typename T, int HD, bool kSwizzled>
-__global__ void __launch_bounds__(kCombineThreads) attend_paged_combine_kernel(const Plan p, const long long* cuts,
+__global__ void __launch_bounds__(kCombineThreads) attend_paged_combine_kernel(const Plan p, const Cut* cuts,
                                                                                const float* partial, T* out, int n_q_heads,
                                                                                int ctas) {
-    __shared__ long long begin[EC_PAGED_MAX_BATCH + 1];
+    // rows / (parts - 1), rounded up, times parts: most for two parts of 256 rows, or one row of as many parts as there are CTAs
+    __shared__ float weight[kMaxWeights];
+    __shared__ int run[2];
     const int c = blockIdx.x + 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    // (the lengths are the caller's, complete before the first launch: laid out while that one still runs)
     tc::pdl_wait();
     tc::pdl_launch_dependents();
-    const long long w = cuts[c], all = cuts[ctas];
-    if (w >= all || w == cuts[c - 1]) return;   // no work behind the cut, or the same cut as the one before
-    Plan quiet = p;
-    quiet.dev_status = nullptr;
-    lay_out(quiet, begin);
-    const Unit u = unit_at(quiet, begin, w);
-    if (w == u.w0) return;   // between two units
-    const long long end = u.w0 + u.steps;
-    int lo = c, hi = c;      // cuts inside the unit; part i runs from cut i to cut i + 1
-    while (cuts[lo - 1] > u.w0) --lo;
-    while (hi + 1 <= ctas && cuts[hi + 1] < end) ++hi;
+    const Cut u = cuts[c];
+    if (u.w0 < 0 || u.w == u.w0) return;   // nothing behind the cut, or it stands between two units
+    // the cuts that divide the same unit are the CTAs' around this one: warp 0 looks down, warp 1 up
+    if (warp < 2) {
+        const int step = warp == 0 ? -1 : 1;
+        int at = c;
+        for (;;) {
+            const int i = at + step * (lane + 1);
+            const bool same = i >= 1 && i <= ctas && cuts[i].w0 == u.w0 && cuts[i].w > u.w0;
+            const uint32_t m = __ballot_sync(0xffffffffu, same);
+            at += step * (m == 0xffffffffu ? 32 : __ffs(~m) - 1);
+            if (m != 0xffffffffu) break;
+        }
+        if (lane == 0) run[warp] = at;
+    }
+    __syncthreads();
+    const int lo = run[0], hi = run[1];   // part i runs from cut lo - 1 + i to the next
     const int sharers = hi - lo + 1, parts = sharers + 1;
-    const long long rows = min((long long)p.tm, (long long)u.s.n * p.group - (long long)u.tile * p.tm);
+    const int rows = (int)min((long long)p.tm, (long long)u.n * p.group - (long long)u.tile * p.tm);
     const long long stride = (long long)p.tm * (HD + 2);
     // part 0 is the worker of the cut before `lo`, its second slot
     auto part_at = [&](int i) { return partial + ((long long)(lo - 1 + i) * 2 + (i == 0 ? 1 : 0)) * stride; };
-    for (long long r = (c - lo) + (long long)warp * sharers; r < rows; r += (long long)sharers * (kCombineThreads / 32)) {
-        float M = -INFINITY;
-        for (int i = lane; i < parts; i += 32) M = fmaxf(M, part_at(i)[p.tm * HD + r * 2]);
-        M = tc::redux_max(M);
-        const float ref = M == -INFINITY ? 0.f : M;
-        float L = 0.f, acc[HD / 32] = {};
-        for (int i0 = 0; i0 < parts; i0 += 32) {
-            float f = 0.f;
-            if (i0 + lane < parts) {
-                const float2 ml = *reinterpret_cast<const float2*>(part_at(i0 + lane) + p.tm * HD + r * 2);
-                f = exp2f(ml.x - ref);
-                L = fmaf(f, ml.y, L);
-            }
-            const int here = min(32, parts - i0);
+    const int per = (rows + sharers - 1) / sharers, row0 = (c - lo) * per, mine = min(per, rows - row0);
+    // the weights of this CTA's rows, one row a thread
+    for (int i = threadIdx.x; i < mine; i += kCombineThreads) {
+        const long long at = (long long)p.tm * HD + (row0 + i) * 2;
+        float M = -INFINITY, L = 0.f;
 #pragma unroll 4
-            for (int i = 0; i < here; ++i) {
-                const float g = __shfl_sync(0xffffffffu, f, i);
-                constexpr int PIECES = HD / 4;
-                int at = lane * (HD / 32);
-                if constexpr (kSwizzled) at = (((at >> 2) ^ ((int)r & (PIECES - 1))) << 2) | (at & 3);
-                const float* src = part_at(i0 + i) + r * HD + at;
+        for (int k = 0; k < parts; ++k) M = fmaxf(M, part_at(k)[at]);
+        const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll 4
+        for (int k = 0; k < parts; ++k) {
+            const float2 ml = *reinterpret_cast<const float2*>(part_at(k) + at);
+            const float f = exp2f(ml.x - ref);
+            L = fmaf(f, ml.y, L);
+            weight[i * parts + k] = f;
+        }
+        const float inv = L > 0.f ? 1.f / L : 0.f;
+        for (int k = 0; k < parts; ++k) weight[i * parts + k] *= inv;
+    }
+    __syncthreads();
+    // the rows, four at a time a warp: their loads are under way together
+    constexpr int C = HD / 32, PIECES = HD / 4, RG = 4;
+    for (int i0 = warp * RG; i0 < mine; i0 += kCombineThreads / 32 * RG) {
+        float acc[RG][C] = {};
+#pragma unroll 2
+        for (int k = 0; k < parts; ++k) {
+            const float* src = part_at(k) + (long long)row0 * HD;
+            float x[RG][C];
+#pragma unroll
+            for (int j = 0; j < RG; ++j) {
+                const int i = min(i0 + j, mine - 1);
+                int at = lane * C;
+                if constexpr (kSwizzled) at = (((at >> 2) ^ ((row0 + i) & (PIECES - 1))) << 2) | (at & 3);
                 if constexpr (HD == 128) {
-                    const float4 x = *reinterpret_cast<const float4*>(src);
-                    acc[0] = fmaf(g, x.x, acc[0]), acc[1] = fmaf(g, x.y, acc[1]);
-                    acc[2] = fmaf(g, x.z, acc[2]), acc[3] = fmaf(g, x.w, acc[3]);
+                    const float4 v = *reinterpret_cast<const float4*>(src + i * HD + at);
+                    x[j][0] = v.x, x[j][1] = v.y, x[j][2] = v.z, x[j][3] = v.w;
                 } else {
-                    const float2 x = *reinterpret_cast<const float2*>(src);
-                    acc[0] = fmaf(g, x.x, acc[0]), acc[1] = fmaf(g, x.y, acc[1]);
+                    const float2 v = *reinterpret_cast<const float2*>(src + i * HD + at);
+                    x[j][0] = v.x, x[j][1] = v.y;
                 }
+            }
+#pragma unroll
+            for (int j = 0; j < RG; ++j) {
+                const float f = weight[min(i0 + j, mine - 1) * parts + k];
+#pragma unroll
+                for (int e = 0; e < C; ++e) acc[j][e] = fmaf(f, x[j][e], acc[j][e]);
             }
         }
 #pragma unroll
-        for (int o = 16; o; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
-        const float inv = L > 0.f ? 1.f / L : 0.f;
-        const long long pr = (long long)u.tile * p.tm + r;
-        T* dst = out + ((u.s.row0 + pr / p.group) * n_q_heads + u.head * p.group + pr % p.group) * HD + lane * (HD / 32);
-        if constexpr (HD == 128) {
-            store4(dst, acc, inv);
-        } else if constexpr (sizeof(T) == 4) {
-            *reinterpret_cast<float2*>(dst) = make_float2(acc[0] * inv, acc[1] * inv);
-        } else {
-            *reinterpret_cast<uint32_t*>(dst) = tc::pack_bf16x2(acc[0] * inv, acc[1] * inv);
+        for (int j = 0; j < RG; ++j) {
+            if (i0 + j >= mine) break;
+            const long long pr = (long long)u.tile * p.tm + row0 + i0 + j;
+            T* dst = out + ((u.row0 + pr / p.group) * n_q_heads + u.head * p.group + pr % p.group) * HD + lane * C;
+            if constexpr (HD == 128) {
+                store4(dst, acc[j], 1.f);
+            } else if constexpr (sizeof(T) == 4) {
+                *reinterpret_cast<float2*>(dst) = make_float2(acc[j][0], acc[j][1]);
+            } else {
+                *reinterpret_cast<uint32_t*>(dst) = tc::pack_bf16x2(acc[j][0], acc[j][1]);
+            }
         }
     }
 }
 
-inline size_t cuts_bytes(int ctas) { return ((size_t)(ctas + 1) * 8 + 127) & ~(size_t)127; }
+inline size_t cuts_bytes(int ctas) { return ((size_t)(ctas + 1) * sizeof(Cut) + 127) & ~(size_t)127; }
 
 inline Plan make_plan(const PagedArgs& a, int tm, int tk) {
     Plan p;
@@ -112,9 +137,10 @@ inline Plan make_plan(const PagedArgs& a, int tm, int tk) {
 }
 
 template <typename T, int HD, bool kSwizzled = false>
-cudaError_t launch_combine(const Plan& p, const long long* cuts, const float* partial, void* out, int n_q_heads, int ctas,
+cudaError_t launch_combine(const Plan& p, const Cut* cuts, const float* partial, void* out, int n_q_heads, int ctas,
                            cudaStream_t stream) {
     if (ctas < 2) return cudaSuccess;
+    if (2 * 256 + 2 * ctas > kMaxWeights) return cudaErrorInvalidValue;   // (a GPU of more than 256 SMs)
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(ctas - 1, 1, 1);
     cfg.blockDim = dim3(kCombineThreads, 1, 1);
