@@ -89,6 +89,31 @@ __device__ __forceinline__ void step_unit(const Plan& p, Unit& u) {
     u.steps = steps_of(p, u.s, u.tile);
 }
 
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+// packed rows of a unit
+__device__ __forceinline__ int rows_of(const Plan& p, const Unit& u) {
+    return (int)min((long long)u.s.n * p.group - (long long)u.tile * (2 * BM), (long long)(2 * BM));
+}
+// Where packed row r of a unit stands: token of the sequence, query head.  Made anew where it is needed: kept, it would cost
+// the softmax registers.
+struct Places {
+    int group, tok0, head0, row0, head;
+    __device__ __forceinline__ Places(const Plan& p, const Unit& unit) {
+        const volatile Unit& u = unit;
+        group = p.group;
+        const long long first = (long long)u.tile * (2 * BM);
+        tok0 = (int)(first / group);
+        head0 = (int)(first - (long long)tok0 * group);
+        row0 = u.s.row0;
+        head = u.head;
+    }
+    __device__ __forceinline__ int token(int r) const { return tok0 + (head0 + r) / group; }
+    __device__ __forceinline__ long long element(int r, int n_q_heads, int hd) const {   // of q and out
+        const unsigned pr = head0 + r, tok = pr / (unsigned)group, hh = pr - tok * group;
+        return ((long long)(row0 + tok0 + (int)tok) * n_q_heads + head * group + (int)hh) * hd;
+    }
+};
+
 template <int HD>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Params p) {
@@ -163,11 +188,9 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
 
     for (int at = 0; segments[at].more; at ^= 1) {
         const Segment& seg = segments[at];
-        const int j0 = seg.j0, T = seg.j1 - j0, kv = seg.u.s.kv;
-        const int group = p.plan.group;
-        const long long r_pair = (long long)seg.u.tile * (2 * BM);
-        const int rows = (int)min((long long)seg.u.s.n * group - r_pair, (long long)(2 * BM));   // of this unit
-        const int tok0 = (int)(r_pair / group), head0 = (int)(r_pair - (long long)tok0 * group);   // of its first row
+        // (values out of shared memory are not warp-uniform to the compiler, and then neither is anything in a loop over them: see
+        // elect_one on what that costs the issuer)
+        const int j0 = uniform(seg.j0), T = uniform(seg.j1) - j0, kv = uniform(seg.u.s.kv), rows = uniform(rows_of(p.plan, seg.u));
         const int n_tiles_q = rows > BM ? 2 : 1;
         // One row tile: the two halves of the CTA take its even and its odd key tiles, each with a reference and an accumulator of
         // its own, so that the softmax of one tile runs under the products of the other; the rows are joined at the end.
@@ -299,6 +322,7 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                         const int t = j & 1;
                         const uint64_t desc_v = smem_desc(base + OFF_RING + take(false) * TILE, SUB, 1024);
                         if (j == j_end) zeroed(pass);
+#pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             mbar_wait_warp(bar(B_PFULL + h * 2 + t), (p_phase >> t) & 1, abort_flag, dev_status);
                             fence_after();
@@ -370,35 +394,33 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
             auto piece = [&](int rw, int g) {   // 16-byte piece g of a row of the row tile: 128-byte swizzle
                 return reinterpret_cast<uint4*>(qtile + (g >> 3) * SUB + (rw >> 3) * 1024 + (rw & 7) * 128 + (((g & 7) ^ (rw & 7)) << 4));
             };
-            // first element of packed row r of the unit (r < rows)
-            auto place = [&](int r) -> long long {
-                const unsigned pr = head0 + r, tok = pr / (unsigned)group, hh = pr - tok * group;
-                return ((long long)(seg.u.s.row0 + tok0 + (int)tok) * p.n_q_heads + seg.u.head * group + (int)hh) * HD;
-            };
             constexpr int RW = 32 / CH;   // rows at a time, CH lanes a half row
             const int sub = lane / CH, ch = lane % CH;
             if (t < n_chains) {
                 const int tq = split ? 0 : t;              // row tile
                 const int js = split ? 2 : 1;              // key tiles jt, jt + js, ...: nt of them
                 const int jt = split ? t : 0, nt = (T - jt + js - 1) / js;
-                // ---- Q: a warp its 32 rows, its half of the columns ----
-                if (tq == t) {
-                    uint4 x[CH];
+                int lim;   // keys that this row sees (rows behind the last: what the sequence has)
+                {
+                    const Places places(p.plan, seg.u);
+                    // ---- Q: a warp its 32 rows, its half of the columns ----
+                    if (tq == t) {
+                        uint4 x[CH];
 #pragma unroll
-                    for (int k = 0; k < CH; ++k) {
-                        const int r = t * BM + quarter * 32 + k * RW + sub;
-                        x[k] = make_uint4(0, 0, 0, 0);
-                        if (r < rows) x[k] = *reinterpret_cast<const uint4*>(p.q + place(r) + h * CW + ch * 8);
+                        for (int k = 0; k < CH; ++k) {
+                            const int r = t * BM + quarter * 32 + k * RW + sub;
+                            x[k] = make_uint4(0, 0, 0, 0);
+                            if (r < rows) x[k] = *reinterpret_cast<const uint4*>(p.q + places.element(r, p.n_q_heads, HD) + h * CW + ch * 8);
+                        }
+#pragma unroll
+                        for (int k = 0; k < CH; ++k) *piece(quarter * 32 + k * RW + sub, h * CH + ch) = x[k];
+                        fence_async_smem();
+                        mbar_arrive(bar(B_QFULL + t));
                     }
-#pragma unroll
-                    for (int k = 0; k < CH; ++k) *piece(quarter * 32 + k * RW + sub, h * CH + ch) = x[k];
-                    fence_async_smem();
-                    mbar_arrive(bar(B_QFULL + t));
+                    const int r = tq * BM + row;
+                    lim = r < rows ? limit_of(p.plan, seg.u.s, places.token(r)) : kv;
                 }
-                // keys that this row sees (rows behind the last: what the sequence has), and the fewest of the warp's
-                const int r_mine = tq * BM + row;
-                const int lim = r_mine < rows ? limit_of(p.plan, seg.u.s, tok0 + (head0 + r_mine) / group) : kv;
-                const int lim_low = __reduce_min_sync(0xffffffffu, lim);
+                const int lim_low = __reduce_min_sync(0xffffffffu, lim);   // the fewest of the warp's rows
                 float m_used = 0.f, l_run = 0.f;
                 const float sl2 = p.scale_log2;
                 const f32x2 sl2_2 = pk(sl2, sl2);
@@ -604,11 +626,12 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                     }
                     __syncwarp();
                     if (!*abort_flag) {   // a CTA whose wait gave up stores nothing
+                        const Places places(p.plan, seg.u);
 #pragma unroll
                         for (int k = 0; k < CH; ++k) {
                             const int rw = quarter * 32 + k * RW + sub, r = t * BM + rw;
                             const uint4 w = *piece(rw, h * CH + ch);
-                            if (r < rows) *reinterpret_cast<uint4*>(p.out + place(r) + h * CW + ch * 8) = w;
+                            if (r < rows) *reinterpret_cast<uint4*>(p.out + places.element(r, p.n_q_heads, HD) + h * CW + ch * 8) = w;
                         }
                     }
                 } else if (writes) {
