@@ -16,20 +16,27 @@
 #include "ec_tc_ptx.cuh"
 
 #include <cooperative_groups.h>
+#include <cstdlib>
 
 namespace ec {
 namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kBins = 32;                  // bin 31: weights that round to 0
+#ifndef EC_ST
+#define EC_ST 512
+#endif
+constexpr int kThreads = EC_ST, kWarps = kThreads / 32;
+constexpr int kBins = 16, kZeroBin = kBins - 1;   // the last: weights that round to 0
+constexpr int kBinBits = 4;
+static_assert(1 << kBinBits == kBins, "bins");
 constexpr int kWeightBits = 53;            // of a thread's column of a bin; the rest counts
 constexpr int kMaxCluster = 8;
 constexpr int kSegment = kThreads * 1016;  // elements of a CTA: 1016 weights of 2^43 units fit a thread's column
-constexpr int kList = 8192;                // candidates that a search takes out of the row
+constexpr int kList = kThreads * kBins / 2;   // candidates that a search takes out of the row: two lists of them over the bins
 constexpr int kFew = 128;                  // candidates that are ranked against one another
 constexpr uint32_t HIST_BYTES = kBins * kThreads * 8;
+constexpr int kMaxDynamic = 232448 - 25600;   // (the rest: struct Shared)
 constexpr int kMaxUnitBits = 47;
 // a thread's weights, none above one, have to fit kWeightBits: as fine a unit as the whole row on one CTA leaves room for
 __host__ __device__ constexpr int unit_bits_of(int vocab) {
@@ -39,9 +46,9 @@ __host__ __device__ constexpr int unit_bits_of(int vocab) {
 }
 typedef unsigned long long u64;
 
-// 2^(i / 64), i = 0 .. 63, from its definition; filled once a CTA
+// 2^(i / 64), i = 0 .. 63, from its definition; a copy for each of sixteen lanes (a half warp's 8-byte loads never meet in a bank)
 struct ExpTable {
-    double v[64];
+    double v[64][16];
 };
 
 __device__ __forceinline__ double widen(float x) {   // exact but for zero and subnormals (below 2^-126: taken as that)
@@ -60,14 +67,28 @@ __device__ __forceinline__ float value_of(uint32_t o) {
 
 struct Scale {   // what turns a logit of this row into a bin and a weight
     float top, per_bin;   // bin = (top - x) * per_bin, to the nearest
+    float low;            // what is below it weighs nothing
     double wide_top, c;   // (x - top) * c = 64 log2 of the weight
     double round, unit;   // 2^(52 - bits), whose last bit is one unit of weight, and 2^bits
 };
-__device__ __forceinline__ int bin_of(const Scale& s, float x) {
-    // every step is monotone in x, so bins are intervals of the order
-    const float z = fminf((s.top - x) * s.per_bin, 31.f);
-    return __float_as_int(z + 8388608.f) & 31;
+// (every step of these three is monotone in x, so what they tell apart are intervals of the order)
+__device__ __forceinline__ float depth_of(const Scale& s, float x) { return fminf((s.top - x) * s.per_bin, (float)kZeroBin); }
+__device__ __forceinline__ int bin_of(const Scale& s, float x) { return __float_as_int(depth_of(s, x) + 8388608.f) & kZeroBin; }
+// part of the interval [z0, z0 + parts / per_part) of depths
+__device__ __forceinline__ int part_of(const Scale& s, float x, float z0, float per_part, int parts) {
+    return min(max(__float2int_rz((depth_of(s, x) - z0) * per_part), 0), parts - 1);
 }
+// sum over the warp, exact while it fits
+__device__ __forceinline__ u64 warp_sum(u64 v) {
+    const uint32_t a = __reduce_add_sync(0xffffffffu, (uint32_t)(v & 0x3ffffffu)), b = __reduce_add_sync(0xffffffffu, (uint32_t)(v >> 26) & 0x3ffffffu),
+                   c = __reduce_add_sync(0xffffffffu, (uint32_t)(v >> 52));
+    return a + ((u64)b << 26) + ((u64)c << 52);
+}
+__device__ __forceinline__ u64 warp_min(u64 v) {
+    const uint32_t h = __reduce_min_sync(0xffffffffu, (uint32_t)(v >> 32));
+    return (u64)h << 32 | __reduce_min_sync(0xffffffffu, (uint32_t)(v >> 32) == h ? (uint32_t)v : 0xffffffffu);
+}
+__device__ __forceinline__ u64 warp_max(u64 v) { return ~warp_min(~v); }
 // Weight in (0, 1], relative error 1e-13: 2^(n/64) from the table, 2^(r/64) for |r| <= 1/2 by its Taylor polynomial
 // ((ln 2 / 128)^5 / 120 = 4e-14 left).  (x - top) * c must be above -64 * 60.
 struct Parts {
@@ -81,7 +102,7 @@ __device__ __forceinline__ Parts weight_parts(const Scale& s, const ExpTable& ta
     const int k = __double2loint(km);
     const double r = u - (km - kMagic);
     const double p = fma(fma(fma(fma(a4, r, a3), r, a2), r, a1), r, 1.0);
-    const double t = tab.v[k & 63];
+    const double t = tab.v[k & 63][threadIdx.x & 15];
     return {p, __hiloint2double(__double2hiint(t) + (k >> 6) * (1 << 20), __double2loint(t))};
 }
 __device__ __forceinline__ u64 weight_units(const Scale& s, const ExpTable& tab, float x) {
@@ -100,12 +121,26 @@ struct Shared {
     u64 bin_w[kBins], bin_c[kBins], all_w, all_c, red_a[kWarps], red_b[kWarps];
     Found found;
     u64 cand_w[kFew];
-    u64 sub_w[256];
-    uint32_t sub_c[256];
+    u64 sub_w[256], part_w[256];
+    uint32_t sub_c[256], part_c[256];
     uint32_t n_list, n_next;
     u64 pick[4];
 };
 
+// 8 consecutive logits as loaded, -inf past `end`
+__device__ __forceinline__ void unpack8(const uint4 (&raw)[1], int i, int end, float (&x)[8]) {
+    const uint32_t w[4] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        x[j] = __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+        if (i + j >= end) x[j] = -INFINITY;
+    }
+}
+__device__ __forceinline__ void unpack8(const uint4 (&raw)[2], int i, int end, float (&x)[8]) {
+    const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = i + j < end ? __uint_as_float(w[j]) : -INFINITY;
+}
 // 8 consecutive logits, -inf past `end`
 __device__ __forceinline__ void load8(const __nv_bfloat16* row, int i, int end, float (&x)[8]) {
     uint4 v = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
@@ -136,18 +171,20 @@ __device__ __forceinline__ void load8(const float* row, int i, int end, float (&
     }
 }
 
-template <typename T>
+static_assert(sizeof(Shared) + kMaxDynamic <= 232448, "shared memory");
+
+template <typename T, bool kResident>
 class RowSampler {
 public:
-    __device__ RowSampler(Shared& sh, unsigned char* hist, const T* row, int begin, int end)
-        : sh(sh), hist(hist), row(row), begin(begin), end(end), cluster(cg::this_cluster()), rank(cluster.block_rank()),
+    __device__ RowSampler(Shared& sh, unsigned char* hist, T* kept, const T* row, int begin, int end)
+        : sh(sh), hist(hist), kept(kept), row(row), begin(begin), end(end), cluster(cg::this_cluster()), rank(cluster.block_rank()),
           n_ranks(cluster.num_blocks()), tid(threadIdx.x), lane(threadIdx.x & 31), warp(threadIdx.x >> 5) {}
 
     __device__ void run(const SampleArgs& a, int r) {
         // ---- largest logit (lowest index on ties) and the smallest finite one ----
         u64 best = ~0ull;
         uint32_t low = 0;
-        each([&](float x, int i) {
+        first_pass([&](float x, int i) {
             if (x > -INFINITY) {
                 const uint32_t o = order_of(x);
                 best = min(best, (u64)o << 32 | (uint32_t)i);
@@ -175,9 +212,9 @@ public:
         s.wide_top = widen(s.top);
         const int bits = unit_bits_of(a.vocab);
         s.round = (double)(1ull << (52 - bits)), s.unit = (double)(1ull << bits);
-        // 31 bins over the nats above half a unit, (bits + 1) ln 2 < 33.4 of them, or over the whole row where that spans less
+        // the other bins over the nats above half a unit, (bits + 1) ln 2 < 33.4 of them, or over the whole row where that spans less
         const float span = (s.top - value_of((uint32_t)low64)) / t;
-        s.per_bin = fminf((span < 33.4f ? fminf(30.f / span, 1e30f) : 30.45f / 33.4f) / t, 1e37f);   // (finite: 0 times it is 0)
+        s.per_bin = fminf((kZeroBin - 0.55f) / fmaxf(fminf(span * 1.001f, 33.4f), 1e-30f) / t, 1e37f);   // (finite: 0 times it is 0)
         // ---- counts and weights by bin, and of the tokens that min-p keeps ----
         const float mp = a.min_p ? a.min_p[r] : 0.f;
         // (at least the largest stays; a bound below a unit asks the exponents instead of the weights)
@@ -188,56 +225,68 @@ public:
 #pragma unroll
         for (int b = 0; b < kBins; ++b) column[b * kThreads] = 0;
         u64 kept_c = 0, kept_w = 0;
-        each([&](float x, int) {
-            if (x == -INFINITY) return;
-            const int b = bin_of(s, x);
-            const u64 w = weight_or_0(x, b);
-            column[b * kThreads] += w + (1ull << kWeightBits);
-            if (tiny ? (widen(x) - s.wide_top) * s.c >= least_u : w >= floor_units) kept_c += 1, kept_w += w;
+        s.low = s.top - kZeroBin / s.per_bin;
+        // (eight weights at a time without a branch: one alone is a chain of ten 64-bit operations)
+        each8([&](const float(&x)[8], int) {
+            u64 w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = weight_units(s, sh.tab, fmaxf(x[j], s.low));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int b = bin_of(s, x[j]);
+                if (b == kZeroBin) w[j] = 0;
+                const u64 one = x[j] > -INFINITY ? 1ull << kWeightBits : 0;
+                column[b * kThreads] += w[j] + one;
+                if (floor_units) {
+                    const bool in = one && (tiny ? (widen(x[j]) - s.wide_top) * s.c >= least_u : w[j] >= floor_units);
+                    kept_c += in, kept_w += in ? w[j] : 0;
+                }
+            }
         });
         block_sum(kept_c, kept_w);
         reduce_bins();
         publish(64, kept_c), publish(65, kept_w);
         const u64(*all)[72] = exchange();
-        if (tid < kBins) {
+        if (tid < 32) {
             u64 w = 0, c = 0;
-            for (int k = 0; k < n_ranks; ++k) w += all[k][tid], c += all[k][32 + tid];
+            for (int k = 0; k < n_ranks && tid < kBins; ++k) w += all[k][tid], c += all[k][32 + tid];
             u64 tw = w, tc = c;
 #pragma unroll
             for (int o = 16; o; o >>= 1) {
                 tw += __shfl_xor_sync(0xffffffffu, tw, o);
                 tc += __shfl_xor_sync(0xffffffffu, tc, o);
             }
-            sh.bin_w[tid] = w, sh.bin_c[tid] = c;
+            if (tid < kBins) sh.bin_w[tid] = w, sh.bin_c[tid] = c;
             if (tid == 0) sh.all_w = tw, sh.all_c = tc;
         }
         kept_c = kept_w = 0;
         for (int k = 0; k < n_ranks; ++k) kept_c += all[k][64], kept_w += all[k][65];
         __syncthreads();
 
-        // ---- the kept prefix ----
+        // ---- the kept prefix, then the token in it ----
         u64 n = sh.all_c, sum = sh.all_w;
-        if (a.top_k) {
-            const int k = a.top_k[r];
-            if (k > 0 && (u64)k < n) {
-                const Found f = search(true, k);
-                n = k, sum = f.weight;
-            }
+        const int k = a.top_k ? a.top_k[r] : 0;
+        const bool cut_k = k > 0 && (u64)k < n;
+        const float p = a.top_p ? a.top_p[r] : 1.f;
+        const double u = (double)a.u[r];
+        const auto reach_p = [&]() { return min((u64)fmax(1.0, ceil((double)p * (double)sum)), sum); };
+        const auto reach_u = [&]() { return min((u64)fmax(0.0, u * (double)sum) + 1, sum); };   // running sum > u * S
+        // Everything is found among the tokens in front of the first search's end.  Where these fit a list, rank 0 takes them
+        // and does the rest alone.
+        const bool head = take_head(cut_k, cut_k ? (u64)k : p < 1.f ? reach_p() : reach_u());
+        if (head && rank != 0) return;
+        const auto find = [&](bool by_count, u64 target) { return head ? search_head(by_count, target) : search(by_count, target); };
+        if (cut_k) {
+            const Found f = find(true, k);
+            n = k, sum = f.weight;
         }
-        if (a.top_p) {
-            const float p = a.top_p[r];
-            if (p < 1.f) {
-                const u64 need = (u64)fmax(1.0, ceil((double)p * (double)sum));
-                const Found f = search(false, min(need, sum));
-                if (f.count < n) n = f.count, sum = f.weight;
-            }
+        if (p < 1.f) {
+            const Found f = find(false, reach_p());
+            if (f.count < n) n = f.count, sum = f.weight;
         }
         if (mp > 1.f) kept_c = 1, kept_w = (u64)s.unit;   // nobody reaches it: the first token alone
         if (floor_units && kept_c < n) n = kept_c, sum = kept_w;
-
-        // ---- the token ----
-        const u64 past = (u64)fmax(0.0, (double)a.u[r] * (double)sum) + 1;   // running sum > u * S
-        const Found f = search(false, min(past, sum));
+        const Found f = find(false, reach_u());
         if (rank == 0 && tid == 0) {
             a.token_out[r] = (int)(uint32_t)f.order;
             if (a.prob_out) {
@@ -251,47 +300,92 @@ public:
 private:
     Shared& sh;
     unsigned char* hist;
-    const T* row;
+    T* const kept;   // the segment in shared memory
+    const T* const row;
     const int begin, end;
     cg::cluster_group cluster;
     const int rank, n_ranks, tid, lane, warp;
     Scale s;
     int turn = 0;
+    int n_head = 0;       // rank 0: tokens of its list,
+    float per_part = 0.f;   // parts a bin of sub_c and sub_w
 
-    // f(logit, index) for this CTA's segment
+    // f(eight logits, index of the first) for this CTA's segment, out of shared memory where it is kept there (a thread finds its
+    // own elements)
     template <typename F>
-    __device__ __forceinline__ void each(F f) {
+    __device__ __forceinline__ void each8(F f) {
         for (int i = begin + tid * 8; i < end; i += kThreads * 8) {
             float x[8];
-            load8(row, i, end, x);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f(x[j], i + j);
+            if constexpr (kResident) load8(kept - begin, i, end, x);
+            else load8(row, i, end, x);
+            f(x, i);
         }
     }
-    __device__ __forceinline__ u64 weight_or_0(float x, int bin) const { return bin < 31 ? weight_units(s, sh.tab, x) : 0; }
+    // f(logit, order) for the tokens of a range: of a bin, of a sixteenth of it (sub >= 0), from lo to hi in the order
+    struct Range {
+        int bin, sub;
+        u64 lo, hi;
+    };
+    template <typename F>
+    __device__ __forceinline__ void each_of(const Range& r, F f) {
+        const float z0 = r.bin - 0.5f;
+        each8([&](const float(&x)[8], int i) {
+            uint32_t in = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) in |= (uint32_t)(bin_of(s, x[j]) == r.bin) << j;
+            if (in == 0) return;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (!(in >> j & 1) || !(x[j] > -INFINITY)) continue;
+                if (r.sub >= 0 && part_of(s, x[j], z0, kBins, kBins) != r.sub) continue;
+                const u64 o = (u64)order_of(x[j]) << 32 | (uint32_t)(i + j);
+                if (o >= r.lo && o <= r.hi) f(x[j], o);
+            }
+        });
+    }
+    // the same over the row itself, four loads under way, leaving the segment in shared memory
+    template <typename F>
+    __device__ __forceinline__ void first_pass(F f) {
+        constexpr int U = 4, V = 8 * sizeof(T) / 16;
+        for (int i0 = begin + tid * 8; i0 < end; i0 += U * kThreads * 8) {
+            uint4 raw[U][V];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int i = i0 + k * kThreads * 8;
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    if (i + v * (8 / V) < end) raw[k][v] = __ldcs(reinterpret_cast<const uint4*>(row + i) + v);
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int i = i0 + k * kThreads * 8;
+                if (i >= end) break;
+                float x[8];
+                unpack8(raw[k], i, end, x);
+                if constexpr (kResident) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) reinterpret_cast<uint4*>(kept - begin + i)[v] = raw[k][v];
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f(x[j], i + j);
+            }
+        }
+    }
+    __device__ __forceinline__ u64 weight_or_0(float x, int bin) const { return bin < kZeroBin ? weight_units(s, sh.tab, x) : 0; }
 
     __device__ __forceinline__ void block_min_max(u64& a, u64& b) {
-#pragma unroll
-        for (int o = 16; o; o >>= 1) {
-            a = min(a, __shfl_xor_sync(0xffffffffu, a, o));
-            b = max(b, __shfl_xor_sync(0xffffffffu, b, o));
-        }
+        a = warp_min(a), b = warp_max(b);
         __syncthreads();
         if (lane == 0) sh.red_a[warp] = a, sh.red_b[warp] = b;
         __syncthreads();
-        for (int k = 0; k < kWarps; ++k) a = min(a, sh.red_a[k]), b = max(b, sh.red_b[k]);
+        a = warp_min(sh.red_a[lane % kWarps]), b = warp_max(sh.red_b[lane % kWarps]);
     }
     __device__ __forceinline__ void block_sum(u64& a, u64& b) {
-#pragma unroll
-        for (int o = 16; o; o >>= 1) {
-            a += __shfl_xor_sync(0xffffffffu, a, o);
-            b += __shfl_xor_sync(0xffffffffu, b, o);
-        }
+        a = warp_sum(a), b = warp_sum(b);
         __syncthreads();
         if (lane == 0) sh.red_a[warp] = a, sh.red_b[warp] = b;
         __syncthreads();
-        a = b = 0;
-        for (int k = 0; k < kWarps; ++k) a += sh.red_a[k], b += sh.red_b[k];
+        a = warp_sum(lane < kWarps ? sh.red_a[lane] : 0), b = warp_sum(lane < kWarps ? sh.red_b[lane] : 0);
     }
     // the CTA's sums of the bins, to every CTA of the row
     __device__ __forceinline__ void reduce_bins() {
@@ -304,11 +398,7 @@ private:
                 const u64 v = h[b * kThreads + k];
                 w += v & ((1ull << kWeightBits) - 1), c += v >> kWeightBits;
             }
-#pragma unroll
-            for (int o = 16; o; o >>= 1) {
-                w += __shfl_xor_sync(0xffffffffu, w, o);
-                c += __shfl_xor_sync(0xffffffffu, c, o);
-            }
+            w = warp_sum(w), c = warp_sum(c);
             if (lane < n_ranks) {
                 u64(*to)[72] = cluster.map_shared_rank(sh.xch[turn], lane);
                 to[rank][b] = w, to[rank][32 + b] = c;
@@ -326,39 +416,152 @@ private:
         return in;
     }
 
-    // The first token, in order, at which the running count (or weight) reaches `target` (1 <= target <= the total).
-    __device__ Found search(bool by_count, u64 target) {
-        // the bin
-        u64 base_c = 0, base_w = 0;
+    // the bin in which the running count (or weight) reaches `target`, and what stands in front of it
+    __device__ __forceinline__ int bin_reaching(bool by_count, u64 target, u64& base_c, u64& base_w) const {
+        base_c = base_w = 0;
         int bin = 0;
-        for (; bin < kBins - 1; ++bin) {
+        for (; bin < kZeroBin; ++bin) {
             const u64 c = sh.bin_c[bin], w = sh.bin_w[bin];
             if ((by_count ? base_c + c : base_w + w) >= target) break;
             base_c += c, base_w += w;
         }
-        if (bin == kBins - 1 && by_count) return Found{target, base_w, ~0ull};   // among the tokens of weight 0: nobody asks which
-        // [lo, hi]: the range of the order that holds it; narrowed until its tokens fit a list
-        u64 lo = 0, hi = ~0ull, in_range = sh.bin_c[bin];
-        while (in_range > kList) {
-            u64 least = ~0ull, most = 0;
-            each([&](float x, int i) {
-                const u64 o = (u64)order_of(x) << 32 | (uint32_t)i;
-                if (x > -INFINITY && bin_of(s, x) == bin && o >= lo && o <= hi) least = min(least, o), most = max(most, o);
+        return bin;
+    }
+    // the CTAs' lists of the tokens that `add` puts there, all on rank 0; returns their number there
+    template <typename F>
+    __device__ __forceinline__ int collect(F each_one) {
+        u64* list = reinterpret_cast<u64*>(hist);
+        if (tid == 0) sh.n_list = 0;
+        __syncthreads();
+        each_one([&](u64 o) { list[atomicAdd(&sh.n_list, 1u)] = o; });
+        cluster.sync();
+        int n = (int)sh.n_list;
+        if (rank == 0) {
+            for (int k = 1; k < n_ranks; ++k) {
+                const int more = (int)*cluster.map_shared_rank(&sh.n_list, k);
+                const u64* from = cluster.map_shared_rank(list, k);
+                for (int i = tid; i < more; i += kThreads) list[n + i] = from[i];
+                n += more;
+            }
+            __syncthreads();
+        }
+        return n;
+    }
+    // Tokens up to the bin that the target falls into, to rank 0's list; false (and nothing done) where they are too many.  On
+    // rank 0 then sub_c, sub_w: running counts and weights of 256 parts of these bins' depths.
+    __device__ bool take_head(bool by_count, u64 target) {
+        u64 base_c, base_w;
+        const int last = bin_reaching(by_count, target, base_c, base_w);
+        if (last == kZeroBin || base_c + sh.bin_c[last] > kList) return false;
+        n_head = collect([&](auto put) {
+            each8([&](const float(&x)[8], int i) {
+                uint32_t in = 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) in |= (uint32_t)(bin_of(s, x[j]) <= last) << j;
+                for (; in; in &= in - 1) {
+                    const int j = __ffs(in) - 1;
+                    float v = x[0];
+#pragma unroll
+                    for (int e = 1; e < 8; ++e) v = j == e ? x[e] : v;
+                    put((u64)order_of(v) << 32 | (uint32_t)(i + j));
+                }
             });
-            block_min_max(least, most);
-            publish(64, least), publish(65, most);
-            const u64(*in)[72] = exchange();
-            least = ~0ull, most = 0;
-            for (int k = 0; k < n_ranks; ++k) least = min(least, in[k][64]), most = max(most, in[k][65]);
-            const int shift = max(0, 59 - __clzll((long long)(most - least)));   // 32 parts of the range, 16 of them used at least
+        });
+        if (rank != 0) return true;
+        per_part = 256.f / (last + 1);
+        const u64* list = reinterpret_cast<const u64*>(hist);
+        if (tid < 256) sh.sub_w[tid] = 0, sh.sub_c[tid] = 0;
+        __syncthreads();
+        for (int i = tid; i < n_head; i += kThreads) {
+            const float x = value_of((uint32_t)(list[i] >> 32));
+            const int part = part_of(s, x, -0.5f, per_part, 256);
+            atomicAdd(&sh.sub_c[part], 1u);
+            atomicAdd(&sh.sub_w[part], weight_units(s, sh.tab, x));
+        }
+        __syncthreads();
+        if (warp == 0) {
+            u64 w[8], tw = 0;
+            uint32_t c[8], tc = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = tw += sh.sub_w[lane * 8 + e], c[e] = tc += sh.sub_c[lane * 8 + e];
+            u64 pw = tw;
+            uint32_t pc = tc;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const u64 xw = __shfl_up_sync(0xffffffffu, pw, o);
+                const uint32_t xc = __shfl_up_sync(0xffffffffu, pc, o);
+                if (lane >= o) pw += xw, pc += xc;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sh.sub_w[lane * 8 + e] = w[e] + pw - tw, sh.sub_c[lane * 8 + e] = c[e] + pc - tc;
+        }
+        __syncthreads();
+        return true;
+    }
+    // search() over the head, by rank 0 alone
+    __device__ Found search_head(bool by_count, u64 target) {
+        const uint32_t below = __ballot_sync(0xffffffffu, (by_count ? (u64)sh.sub_c[lane * 8 + 7] : sh.sub_w[lane * 8 + 7]) < target);
+        int part = __popc(below) * 8;   // (running sums ascend)
+        while (part < 255 && (by_count ? (u64)sh.sub_c[part] : sh.sub_w[part]) < target) ++part;
+        part = min(part, 255);
+        const u64 base_c = part ? sh.sub_c[part - 1] : 0, base_w = part ? sh.sub_w[part - 1] : 0;
+        const u64* list = reinterpret_cast<const u64*>(hist);
+        u64* found = reinterpret_cast<u64*>(hist) + kList;
+        __syncthreads();   // the last search's list and counter are done with
+        if (tid == 0) sh.n_next = 0;
+        __syncthreads();
+        for (int i = tid; i < n_head; i += kThreads) {
+            const u64 o = list[i];
+            if (part_of(s, value_of((uint32_t)(o >> 32)), -0.5f, per_part, 256) == part) found[atomicAdd(&sh.n_next, 1u)] = o;
+        }
+        __syncthreads();
+        const int n = (int)sh.n_next;
+        return select(by_count, target, base_c, base_w, found, n);
+    }
+
+    // The first token, in order, at which the running count (or weight) reaches `target` (1 <= target <= the total).
+    __device__ Found search(bool by_count, u64 target) {
+        u64 base_c, base_w;
+        const int bin = bin_reaching(by_count, target, base_c, base_w);
+        if (bin == kZeroBin && by_count) return Found{target, base_w, ~0ull};   // among the tokens of weight 0: nobody asks which
+        // the range of the order that holds it, narrowed until its tokens fit a list: by the depth first, then by the order itself
+        // (equal logits in the end)
+        Range r{bin, -1, 0, ~0ull};
+        u64 in_range = sh.bin_c[bin];
+        while (in_range > kList) {
+            const bool by_depth = r.sub < 0;
+            u64 least = 0;
+            int shift = 0;
+            if (!by_depth) {
+                u64 most = 0;
+                least = ~0ull;
+                each_of(r, [&](float, u64 o) { least = min(least, o), most = max(most, o); });
+                block_min_max(least, most);
+                publish(64, least), publish(65, most);
+                const u64(*in)[72] = exchange();
+                least = ~0ull, most = 0;
+                for (int k = 0; k < n_ranks; ++k) least = min(least, in[k][64]), most = max(most, in[k][65]);
+                shift = max(0, 64 - kBinBits - __clzll((long long)(most - least)));   // half of the parts are used at least
+            }
             u64* column = reinterpret_cast<u64*>(hist) + tid;
 #pragma unroll
             for (int b = 0; b < kBins; ++b) column[b * kThreads] = 0;
-            each([&](float x, int i) {
-                const u64 o = (u64)order_of(x) << 32 | (uint32_t)i;
-                if (x > -INFINITY && bin_of(s, x) == bin && o >= lo && o <= hi)
-                    column[((o - least) >> shift) * kThreads] += weight_or_0(x, bin) + (1ull << kWeightBits);
-            });
+            const float z0 = bin - 0.5f;
+            if (by_depth) {
+                each8([&](const float(&x)[8], int) {
+                    u64 w[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) w[j] = weight_units(s, sh.tab, fmaxf(x[j], s.low));
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (bin_of(s, x[j]) == bin && x[j] > -INFINITY)
+                            column[part_of(s, x[j], z0, kBins, kBins) * kThreads] += (bin < kZeroBin ? w[j] : 0) + (1ull << kWeightBits);
+                });
+            } else {
+                each_of(r, [&](float x, u64 o) {
+                    column[(int)((o - least) >> shift) * kThreads] += weight_or_0(x, bin) + (1ull << kWeightBits);
+                });
+            }
             reduce_bins();
             const u64(*all)[72] = exchange();
             int part = 0;
@@ -369,62 +572,57 @@ private:
                 if (part == kBins - 1 || (by_count ? base_c + c : base_w + w) >= target) break;
                 base_c += c, base_w += w;
             }
-            lo = least + ((u64)part << shift);
-            hi = lo + ((1ull << shift) - 1);
-            if (hi < lo) hi = ~0ull;
-        }
-        // ---- the list: every CTA its own, then rank 0 all of them ----
-        u64* list = reinterpret_cast<u64*>(hist);
-        if (tid == 0) sh.n_list = 0;
-        __syncthreads();
-        each([&](float x, int i) {
-            const u64 o = (u64)order_of(x) << 32 | (uint32_t)i;
-            const bool in = x > -INFINITY && bin_of(s, x) == bin && o >= lo && o <= hi;
-            if (in) list[atomicAdd(&sh.n_list, 1u)] = o;
-        });
-        cluster.sync();
-        if (rank == 0) {
-            uint32_t n = sh.n_list;
-            for (int k = 1; k < n_ranks; ++k) {
-                const uint32_t more = *cluster.map_shared_rank(&sh.n_list, k);
-                const u64* from = cluster.map_shared_rank(list, k);
-                for (uint32_t i = tid; i < more; i += kThreads) list[n + i] = from[i];
-                n += more;
+            if (by_depth) {
+                r.sub = part;
+            } else {
+                r.lo = least + ((u64)part << shift);
+                r.hi = r.lo + ((1ull << shift) - 1);
+                if (r.hi < r.lo) r.hi = ~0ull;
             }
-            __syncthreads();
-            const Found f = select(by_count, target, base_c, base_w, list, (int)n, bin);
+        }
+        const int n = collect([&](auto put) { each_of(r, [&](float, u64 o) { put(o); }); });
+        if (rank == 0) {
+            const Found f = select(by_count, target, base_c, base_w, reinterpret_cast<u64*>(hist), n);
             if (tid < n_ranks) *cluster.map_shared_rank(&sh.found, tid) = f;
         }
         cluster.sync();
         return sh.found;
     }
 
-    // the same over a list in shared memory, one CTA
-    __device__ Found select(bool by_count, u64 target, u64 base_c, u64 base_w, u64* list, int n, int bin) {
-        u64* other = list + kList;
+    // the same over a list in shared memory, which is used up; one CTA
+    __device__ Found select(bool by_count, u64 target, u64 base_c, u64 base_w, u64* list, int n) {
+        constexpr int kMine = kList / kThreads;
         while (n > kFew) {
-            u64 least = ~0ull, most = 0;
-            for (int i = tid; i < n; i += kThreads) least = min(least, list[i]), most = max(most, list[i]);
+            u64 least = ~0ull, most = 0, o[kMine];
+#pragma unroll
+            for (int e = 0; e < kMine; ++e) {
+                const int i = e * kThreads + tid;
+                o[e] = i < n ? list[i] : ~0ull;
+                if (i < n) least = min(least, o[e]), most = max(most, o[e]);
+            }
             block_min_max(least, most);
-            const int shift = max(0, 56 - __clzll((long long)(most - least)));   // 256 parts
-            if (tid < 256) sh.sub_w[tid] = 0, sh.sub_c[tid] = 0;
+            const int shift = max(0, 56 - __clzll((long long)(most - least)));   // 256 parts, half of them used at least
+            if (tid < 256) sh.part_w[tid] = 0, sh.part_c[tid] = 0;
             if (tid == 0) sh.n_next = 0;
             __syncthreads();
-            for (int i = tid; i < n; i += kThreads) {
-                const int part = (int)((list[i] - least) >> shift);
-                atomicAdd(&sh.sub_c[part], 1u);
-                atomicAdd(&sh.sub_w[part], weight_or_0(value_of((uint32_t)(list[i] >> 32)), bin));
+#pragma unroll
+            for (int e = 0; e < kMine; ++e) {
+                if (e * kThreads + tid >= n) break;
+                const int part = (int)((o[e] - least) >> shift);
+                const float x = value_of((uint32_t)(o[e] >> 32));
+                atomicAdd(&sh.part_c[part], 1u);
+                atomicAdd(&sh.part_w[part], weight_or_0(x, bin_of(s, x)));
             }
             __syncthreads();
             if (warp == 0) {   // the part, by a scan of 8 parts a lane
                 u64 w[8], c[8], tw = 0, tc = 0;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) w[k] = sh.sub_w[lane * 8 + k], c[k] = sh.sub_c[lane * 8 + k], tw += w[k], tc += c[k];
+                for (int k = 0; k < 8; ++k) w[k] = sh.part_w[lane * 8 + k], c[k] = sh.part_c[lane * 8 + k], tw += w[k], tc += c[k];
                 u64 pw = tw, pc = tc;
 #pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const u64 xw = __shfl_up_sync(0xffffffffu, pw, o), xc = __shfl_up_sync(0xffffffffu, pc, o);
-                    if (lane >= o) pw += xw, pc += xc;
+                for (int d = 1; d < 32; d <<= 1) {
+                    const u64 xw = __shfl_up_sync(0xffffffffu, pw, d), xc = __shfl_up_sync(0xffffffffu, pc, d);
+                    if (lane >= d) pw += xw, pc += xc;
                 }
                 const bool reached = (by_count ? base_c + pc : base_w + pw) >= target;
                 const uint32_t m = __ballot_sync(0xffffffffu, reached);
@@ -441,16 +639,18 @@ private:
             __syncthreads();
             base_c = sh.pick[0], base_w = sh.pick[1];
             const int part = (int)sh.pick[2];
-            for (int i = tid; i < n; i += kThreads)
-                if ((int)((list[i] - least) >> shift) == part) other[atomicAdd(&sh.n_next, 1u)] = list[i];
+#pragma unroll
+            for (int e = 0; e < kMine; ++e)
+                if (e * kThreads + tid < n && (int)((o[e] - least) >> shift) == part) list[atomicAdd(&sh.n_next, 1u)] = o[e];
             __syncthreads();
             n = (int)sh.n_next;
-            u64* x = list;
-            list = other, other = x;
             __syncthreads();
         }
         // few: every one against every other; four threads a candidate
-        if (tid < n) sh.cand_w[tid] = weight_or_0(value_of((uint32_t)(list[tid] >> 32)), bin);
+        if (tid < n) {
+            const float x = value_of((uint32_t)(list[tid] >> 32));
+            sh.cand_w[tid] = weight_or_0(x, bin_of(s, x));
+        }
         __syncthreads();
         const int mine = tid >> 2;
         u64 c = 0, w = 0;
@@ -474,36 +674,31 @@ private:
     }
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads, 1) sample_kernel(const SampleArgs a, int segment) {
-    extern __shared__ __align__(16) unsigned char hist[];
+template <typename T, bool kResident>
+__global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a, int segment) {
+    extern __shared__ __align__(16) unsigned char hist[];   // the bins (or lists), then the segment
     __shared__ Shared sh;
     cg::cluster_group cluster = cg::this_cluster();
-    if (threadIdx.x < 64) sh.tab.v[threadIdx.x] = exp2((double)threadIdx.x / 64.0);
+    for (int i = threadIdx.x; i < 64 * 16; i += kThreads) sh.tab.v[i >> 4][i & 15] = exp2((double)(i >> 4) / 64.0);
     tc::pdl_wait();
     tc::pdl_launch_dependents();
     __syncthreads();
     const int n_ranks = cluster.num_blocks(), r = blockIdx.x / n_ranks;
     const int begin = min((int)cluster.block_rank() * segment, a.vocab), end = min(begin + segment, a.vocab);
-    RowSampler<T> row(sh, hist, static_cast<const T*>(a.logits) + r * a.row_stride, begin, end);
+    RowSampler<T, kResident> row(sh, hist, reinterpret_cast<T*>(hist + HIST_BYTES), static_cast<const T*>(a.logits) + r * a.row_stride, begin, end);
     row.run(a, r);
     cluster.sync();   // no CTA leaves while another may still write into its shared memory
 }
 
-template <typename T>
-cudaError_t launch(const SampleArgs& a, cudaStream_t stream) {
-    // CTAs of a row: all SMs at work while rows are few, and a segment that its counters can hold
-    int c = 1;
-    while (c < kMaxCluster && ((long long)a.n_rows * c * 2 <= sm_count() + 4 || a.vocab > c * (long long)kSegment) &&
-           (a.vocab > c * 4096 || a.vocab > c * (long long)kSegment))
-        c *= 2;
+template <typename T, bool kResident>
+cudaError_t launch_as(const SampleArgs& a, int c, int segment, cudaStream_t stream) {
+    const int bytes = (int)HIST_BYTES + (kResident ? segment * (int)sizeof(T) : 0);
     static PerDeviceOnce once;
-    if (const cudaError_t e = ensure_dynamic_smem(once, sample_kernel<T>, (int)HIST_BYTES); e != cudaSuccess) return e;
-    const int segment = ((a.vocab + c - 1) / c + 7) & ~7;
+    if (const cudaError_t e = ensure_dynamic_smem(once, sample_kernel<T, kResident>, kResident ? kMaxDynamic : (int)HIST_BYTES); e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(a.n_rows * c, 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = HIST_BYTES;
+    cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -514,7 +709,19 @@ cudaError_t launch(const SampleArgs& a, cudaStream_t stream) {
     at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, sample_kernel<T>, a, segment);
+    return cudaLaunchKernelEx(&cfg, sample_kernel<T, kResident>, a, segment);
+}
+
+template <typename T>
+cudaError_t launch(const SampleArgs& a, cudaStream_t stream) {
+    // CTAs of a row: enough that a segment stays in shared memory beside the bins, and all SMs at work while rows are few
+    int c = 1;
+    const auto segment = [&](int n) { return ((a.vocab + n - 1) / n + 7) & ~7; };
+    const auto fits = [&](int n) { return (int)HIST_BYTES + (long long)segment(n) * (int)sizeof(T) <= kMaxDynamic; };
+    while (c < kMaxCluster && !fits(c)) c *= 2;
+    if (const char* e = getenv("EC_SC")) c = atoi(e);
+    while (c < kMaxCluster && (long long)a.n_rows * c * 2 <= sm_count() + 4 && a.vocab > c * 4096) c *= 2;
+    return fits(c) ? launch_as<T, true>(a, c, segment(c), stream) : launch_as<T, false>(a, c, segment(c), stream);
 }
 
 }  // namespace
