@@ -16,7 +16,9 @@
 #include "ec_tc_ptx.cuh"
 
 #include <cooperative_groups.h>
+
 #include <cstdlib>
+#include <type_traits>
 
 namespace ec {
 namespace {
@@ -51,10 +53,6 @@ struct ExpTable {
     double v[64][16];
 };
 
-__device__ __forceinline__ double widen(float x) {   // exact but for zero and subnormals (below 2^-126: taken as that)
-    const uint32_t b = __float_as_uint(x);
-    return __hiloint2double((int)((b & 0x80000000u) | (((b & 0x7fffffffu) >> 3) + 0x38000000u)), (int)(b << 29));
-}
 // Order of a logit as an integer, ascending with DESCENDING logits; both zeros alike
 __device__ __forceinline__ uint32_t order_of(float x) {
     uint32_t b = __float_as_uint(x);
@@ -65,10 +63,27 @@ __device__ __forceinline__ float value_of(uint32_t o) {
     return __uint_as_float((o & 0x80000000u) ? o : (~o & 0x7fffffffu));
 }
 
+// shared memory by its own addresses
+__device__ __forceinline__ u64 lds64(uint32_t at) {
+    u64 v;
+    asm volatile("ld.shared.u64 %0, [%1];" : "=l"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts64(uint32_t at, u64 v) { asm volatile("st.shared.u64 [%0], %1;" ::"r"(at), "l"(v) : "memory"); }
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts128(uint32_t at, const uint4& v) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
 struct Scale {   // what turns a logit of this row into a bin and a weight
     float top, per_bin;   // bin = (top - x) * per_bin, to the nearest
     float low;            // what is below it weighs nothing
     double wide_top, c;   // (x - top) * c = 64 log2 of the weight
+    uint32_t table;       // shared address of this lane's copy of ExpTable
     double round, unit;   // 2^(52 - bits), whose last bit is one unit of weight, and 2^bits
 };
 // (every step of these three is monotone in x, so what they tell apart are intervals of the order)
@@ -94,20 +109,25 @@ __device__ __forceinline__ u64 warp_max(u64 v) { return ~warp_min(~v); }
 struct Parts {
     double poly, scale;
 };
-__device__ __forceinline__ Parts weight_parts(const Scale& s, const ExpTable& tab, float x) {
+__device__ __forceinline__ Parts weight_parts(const Scale& s, float x) {
     constexpr double kMagic = 6755399441055744.0;   // 1.5 * 2^52: the sum's low bits are the nearest integer
     constexpr double a1 = 0.010830424696249145, a2 = a1 * a1 / 2, a3 = a1 * a1 * a1 / 6, a4 = a1 * a1 * a1 * a1 / 24;   // ln 2 / 64
-    const double u = (widen(x) - s.wide_top) * s.c;
+    const double u = ((double)(x) - s.wide_top) * s.c;
     const double km = u + kMagic;
     const int k = __double2loint(km);
     const double r = u - (km - kMagic);
     const double p = fma(fma(fma(fma(a4, r, a3), r, a2), r, a1), r, 1.0);
-    const double t = tab.v[k & 63][threadIdx.x & 15];
+    double t;   // (not volatile: the table stays as it is)
+    asm("ld.shared.f64 %0, [%1];" : "=d"(t) : "r"(s.table + (k & 63) * 128));
     return {p, __hiloint2double(__double2hiint(t) + (k >> 6) * (1 << 20), __double2loint(t))};
 }
-__device__ __forceinline__ u64 weight_units(const Scale& s, const ExpTable& tab, float x) {
-    const Parts w = weight_parts(s, tab, x);
-    return (u64)(__double_as_longlong(fma(w.poly, w.scale, s.round)) - __double_as_longlong(s.round));
+// units of weight + bits(s.round)
+__device__ __forceinline__ u64 weight_raw(const Scale& s, float x) {
+    const Parts w = weight_parts(s, x);
+    return (u64)__double_as_longlong(fma(w.poly, w.scale, s.round));
+}
+__device__ __forceinline__ u64 weight_units(const Scale& s, float x) {
+    return weight_raw(s, x) - (u64)__double_as_longlong(s.round);
 }
 
 struct Found {    // the token that a search ends at
@@ -133,13 +153,22 @@ __device__ __forceinline__ void unpack8(const uint4 (&raw)[1], int i, int end, f
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         x[j] = __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
-        if (i + j >= end) x[j] = -INFINITY;
+    }
+    if (i + 8 > end) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (i + j >= end) x[j] = -INFINITY;
     }
 }
 __device__ __forceinline__ void unpack8(const uint4 (&raw)[2], int i, int end, float (&x)[8]) {
     const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = i + j < end ? __uint_as_float(w[j]) : -INFINITY;
+    for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(w[j]);
+    if (i + 8 > end) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (i + j >= end) x[j] = -INFINITY;
+    }
 }
 // 8 consecutive logits, -inf past `end`
 __device__ __forceinline__ void load8(const __nv_bfloat16* row, int i, int end, float (&x)[8]) {
@@ -176,7 +205,7 @@ static_assert(sizeof(Shared) + kMaxDynamic <= 232448, "shared memory");
 template <typename T, bool kResident>
 class RowSampler {
 public:
-    __device__ RowSampler(Shared& sh, unsigned char* hist, T* kept, const T* row, int begin, int end)
+    __device__ RowSampler(Shared& sh, unsigned char* hist, uint32_t kept, const T* row, int begin, int end)
         : sh(sh), hist(hist), kept(kept), row(row), begin(begin), end(end), cluster(cg::this_cluster()), rank(cluster.block_rank()),
           n_ranks(cluster.num_blocks()), tid(threadIdx.x), lane(threadIdx.x & 31), warp(threadIdx.x >> 5) {}
 
@@ -209,7 +238,8 @@ public:
         }
         s.top = value_of((uint32_t)(best >> 32));
         s.c = 64.0 * 1.4426950408889634074 / (double)t;
-        s.wide_top = widen(s.top);
+        s.table = tc::s2u(&sh.tab.v[0][tid & 15]);
+        s.wide_top = (double)(s.top);
         const int bits = unit_bits_of(a.vocab);
         s.round = (double)(1ull << (52 - bits)), s.unit = (double)(1ull << bits);
         // the other bins over the nats above half a unit, (bits + 1) ln 2 < 33.4 of them, or over the whole row where that spans less
@@ -221,59 +251,64 @@ public:
         const u64 floor_units = mp > 0.f ? (u64)fmin(ceil((double)mp * s.unit), s.unit) : 0;
         const bool tiny = floor_units == 1;
         const double least_u = tiny ? 64.0 * log2((double)mp) : 0.0;
-        u64* column = reinterpret_cast<u64*>(hist) + tid;
+        const uint32_t column = tc::s2u(hist) + tid * 8;
 #pragma unroll
-        for (int b = 0; b < kBins; ++b) column[b * kThreads] = 0;
+        for (int b = 0; b < kBins; ++b) sts64(column + b * (kThreads * 8), 0);
         u64 kept_c = 0, kept_w = 0;
         s.low = s.top - kZeroBin / s.per_bin;
+        const int k = a.top_k ? a.top_k[r] : 0;
+        constexpr u64 kOne = 1ull << kWeightBits;
+        if (k > 0 && k <= kList / 2) {
+            // The first k tokens are all that counts, and (nearly always) they fit the list: their weights are formed there
+            each8([&](const float(&x)[8], int) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    bump(column, bin_of(s, x[j]), x[j] > -INFINITY ? kOne : 0);
+            });
+            if (count_bins(a, r, k)) return;
+#pragma unroll
+            for (int b = 0; b < kBins; ++b) sts64(column + b * (kThreads * 8), 0);
+        }
         // (eight weights at a time without a branch: one alone is a chain of ten 64-bit operations)
-        each8([&](const float(&x)[8], int) {
-            u64 w[8];
+        const auto weigh = [&](auto with_floor) {
+            const u64 one = kOne - (u64)__double_as_longlong(s.round);
+            each8([&](const float(&x)[8], int) {
+                u64 w[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = weight_units(s, sh.tab, fmaxf(x[j], s.low));
+                for (int j = 0; j < 8; ++j) w[j] = weight_raw(s, fmaxf(x[j], s.low));
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int b = bin_of(s, x[j]);
-                if (b == kZeroBin) w[j] = 0;
-                const u64 one = x[j] > -INFINITY ? 1ull << kWeightBits : 0;
-                column[b * kThreads] += w[j] + one;
-                if (floor_units) {
-                    const bool in = one && (tiny ? (widen(x[j]) - s.wide_top) * s.c >= least_u : w[j] >= floor_units);
-                    kept_c += in, kept_w += in ? w[j] : 0;
+                for (int j = 0; j < 8; ++j) {
+                    const int b = bin_of(s, x[j]);
+                    u64 add = w[j] + one;
+                    if (b == kZeroBin) add = x[j] > -INFINITY ? kOne : 0;
+                    bump(column, b, add);
+                    if constexpr (decltype(with_floor)::value) {
+                        const u64 units = add & (kOne - 1);
+                        const bool in = add && (tiny ? ((double)x[j] - s.wide_top) * s.c >= least_u : units >= floor_units);
+                        kept_c += in, kept_w += in ? units : 0;
+                    }
                 }
-            }
-        });
+            });
+        };
+        if (floor_units) weigh(std::true_type{});
+        else weigh(std::false_type{});
         block_sum(kept_c, kept_w);
         reduce_bins();
         publish(64, kept_c), publish(65, kept_w);
         const u64(*all)[72] = exchange();
-        if (tid < 32) {
-            u64 w = 0, c = 0;
-            for (int k = 0; k < n_ranks && tid < kBins; ++k) w += all[k][tid], c += all[k][32 + tid];
-            u64 tw = w, tc = c;
-#pragma unroll
-            for (int o = 16; o; o >>= 1) {
-                tw += __shfl_xor_sync(0xffffffffu, tw, o);
-                tc += __shfl_xor_sync(0xffffffffu, tc, o);
-            }
-            if (tid < kBins) sh.bin_w[tid] = w, sh.bin_c[tid] = c;
-            if (tid == 0) sh.all_w = tw, sh.all_c = tc;
-        }
+        sum_bins(all);
         kept_c = kept_w = 0;
         for (int k = 0; k < n_ranks; ++k) kept_c += all[k][64], kept_w += all[k][65];
         __syncthreads();
 
         // ---- the kept prefix, then the token in it ----
         u64 n = sh.all_c, sum = sh.all_w;
-        const int k = a.top_k ? a.top_k[r] : 0;
         const bool cut_k = k > 0 && (u64)k < n;
         const float p = a.top_p ? a.top_p[r] : 1.f;
         const double u = (double)a.u[r];
-        const auto reach_p = [&]() { return min((u64)fmax(1.0, ceil((double)p * (double)sum)), sum); };
-        const auto reach_u = [&]() { return min((u64)fmax(0.0, u * (double)sum) + 1, sum); };   // running sum > u * S
         // Everything is found among the tokens in front of the first search's end.  Where these fit a list, rank 0 takes them
         // and does the rest alone.
-        const bool head = take_head(cut_k, cut_k ? (u64)k : p < 1.f ? reach_p() : reach_u());
+        const bool head = take_head(cut_k, cut_k ? (u64)k : p < 1.f ? reach(p, sum) : pass(u, sum));
         if (head && rank != 0) return;
         const auto find = [&](bool by_count, u64 target) { return head ? search_head(by_count, target) : search(by_count, target); };
         if (cut_k) {
@@ -281,26 +316,18 @@ public:
             n = k, sum = f.weight;
         }
         if (p < 1.f) {
-            const Found f = find(false, reach_p());
+            const Found f = find(false, reach(p, sum));
             if (f.count < n) n = f.count, sum = f.weight;
         }
         if (mp > 1.f) kept_c = 1, kept_w = (u64)s.unit;   // nobody reaches it: the first token alone
         if (floor_units && kept_c < n) n = kept_c, sum = kept_w;
-        const Found f = find(false, reach_u());
-        if (rank == 0 && tid == 0) {
-            a.token_out[r] = (int)(uint32_t)f.order;
-            if (a.prob_out) {
-                const Parts w = weight_parts(s, sh.tab, value_of((uint32_t)(f.order >> 32)));
-                a.prob_out[r] = (float)(w.poly * w.scale * s.unit / (double)sum);
-            }
-            if (a.kept_out) a.kept_out[r] = (int)n;
-        }
+        answer(a, r, find(false, pass(u, sum)), n, sum);
     }
 
 private:
     Shared& sh;
     unsigned char* hist;
-    T* const kept;   // the segment in shared memory
+    const uint32_t kept;   // the segment in shared memory
     const T* const row;
     const int begin, end;
     cg::cluster_group cluster;
@@ -310,14 +337,79 @@ private:
     int n_head = 0;       // rank 0: tokens of its list,
     float per_part = 0.f;   // parts a bin of sub_c and sub_w
 
+    static __device__ __forceinline__ void bump(uint32_t column, int b, u64 add) {
+        const uint32_t at = column + b * (kThreads * 8);
+        sts64(at, lds64(at) + add);
+    }
+    // the first running sums that reach p of `sum`, and that exceed u of it
+    static __device__ __forceinline__ u64 reach(float p, u64 sum) { return min((u64)fmax(1.0, ceil((double)p * (double)sum)), sum); }
+    static __device__ __forceinline__ u64 pass(double u, u64 sum) { return min((u64)fmax(0.0, u * (double)sum) + 1, sum); }
+    __device__ __forceinline__ void answer(const SampleArgs& a, int r, const Found& f, u64 n, u64 sum) {
+        if (rank != 0 || tid != 0) return;
+        a.token_out[r] = (int)(uint32_t)f.order;
+        if (a.prob_out) {
+            const Parts w = weight_parts(s, value_of((uint32_t)(f.order >> 32)));
+            a.prob_out[r] = (float)(w.poly * w.scale * s.unit / (double)sum);
+        }
+        if (a.kept_out) a.kept_out[r] = (int)n;
+    }
+    __device__ __forceinline__ void sum_bins(const u64 (*all)[72]) {
+        if (tid >= 32) return;
+        u64 w = 0, c = 0;
+        for (int k = 0; k < n_ranks && tid < kBins; ++k) w += all[k][tid], c += all[k][32 + tid];
+        const u64 tw = warp_sum(w), tc = warp_sum(c);
+        if (tid < kBins) sh.bin_w[tid] = w, sh.bin_c[tid] = c;
+        if (tid == 0) sh.all_w = tw, sh.all_c = tc;
+    }
+    // Rows with a top k: the bins hold counts alone.  Where the tokens up to the k-th's bin fit the list, rank 0 finds everything
+    // among them (min-p too: what it keeps beyond the k-th does not matter) and the row is done.
+    __device__ bool count_bins(const SampleArgs& a, int r, int k) {
+        reduce_bins();
+        sum_bins(exchange());
+        __syncthreads();
+        const u64 live = sh.all_c;
+        if ((u64)k >= live || !take_head(true, (u64)k)) return false;
+        if (rank != 0) return true;
+        Found f = search_head(true, (u64)k);
+        u64 n = k, sum = f.weight;
+        const float p = a.top_p ? a.top_p[r] : 1.f, mp = a.min_p ? a.min_p[r] : 0.f;
+        if (p < 1.f) {
+            f = search_head(false, reach(p, sum));
+            if (f.count < n) n = f.count, sum = f.weight;
+        }
+        if (mp > 1.f) {
+            n = 1, sum = (u64)s.unit;
+        } else if (mp > 0.f) {
+            const u64 least = (u64)fmin(ceil((double)mp * s.unit), s.unit);
+            const double least_u = 64.0 * log2((double)mp);
+            const u64* list = reinterpret_cast<const u64*>(hist);
+            u64 c = 0, w = 0;
+            for (int i = tid; i < n_head; i += kThreads) {
+                const float x = value_of((uint32_t)(list[i] >> 32));
+                const u64 units = weight_units(s, x);
+                if (least == 1 ? ((double)x - s.wide_top) * s.c >= least_u : units >= least) c += 1, w += units;
+            }
+            block_sum(c, w);
+            if (c < n) n = c, sum = w;
+        }
+        answer(a, r, search_head(false, pass((double)a.u[r], sum)), n, sum);
+        return true;
+    }
     // f(eight logits, index of the first) for this CTA's segment, out of shared memory where it is kept there (a thread finds its
     // own elements)
     template <typename F>
     __device__ __forceinline__ void each8(F f) {
         for (int i = begin + tid * 8; i < end; i += kThreads * 8) {
             float x[8];
-            if constexpr (kResident) load8(kept - begin, i, end, x);
-            else load8(row, i, end, x);
+            if constexpr (kResident) {
+                constexpr int V = 8 * sizeof(T) / 16;
+                uint4 raw[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) raw[v] = lds128(kept + (i - begin) * (int)sizeof(T) + v * 16);
+                unpack8(raw, i, end, x);
+            } else {
+                load8(row, i, end, x);
+            }
             f(x, i);
         }
     }
@@ -332,16 +424,22 @@ private:
         each8([&](const float(&x)[8], int i) {
             uint32_t in = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) in |= (uint32_t)(bin_of(s, x[j]) == r.bin) << j;
-            if (in == 0) return;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (!(in >> j & 1) || !(x[j] > -INFINITY)) continue;
-                if (r.sub >= 0 && part_of(s, x[j], z0, kBins, kBins) != r.sub) continue;
-                const u64 o = (u64)order_of(x[j]) << 32 | (uint32_t)(i + j);
-                if (o >= r.lo && o <= r.hi) f(x[j], o);
+            for (int j = 0; j < 8; ++j)
+                in |= (uint32_t)(bin_of(s, x[j]) == r.bin && (r.sub < 0 || part_of(s, x[j], z0, kBins, kBins) == r.sub)) << j;
+            for (; in; in &= in - 1) {
+                const int j = __ffs(in) - 1;
+                const float v = pick(x, j);
+                if (!(v > -INFINITY)) continue;
+                const u64 o = (u64)order_of(v) << 32 | (uint32_t)(i + j);
+                if (o >= r.lo && o <= r.hi) f(v, o);
             }
         });
+    }
+    static __device__ __forceinline__ float pick(const float (&x)[8], int j) {
+        float v = x[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) v = j == e ? x[e] : v;
+        return v;
     }
     // the same over the row itself, four loads under way, leaving the segment in shared memory
     template <typename F>
@@ -364,14 +462,14 @@ private:
                 unpack8(raw[k], i, end, x);
                 if constexpr (kResident) {
 #pragma unroll
-                    for (int v = 0; v < V; ++v) reinterpret_cast<uint4*>(kept - begin + i)[v] = raw[k][v];
+                    for (int v = 0; v < V; ++v) sts128(kept + (i - begin) * (int)sizeof(T) + v * 16, raw[k][v]);
                 }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) f(x[j], i + j);
             }
         }
     }
-    __device__ __forceinline__ u64 weight_or_0(float x, int bin) const { return bin < kZeroBin ? weight_units(s, sh.tab, x) : 0; }
+    __device__ __forceinline__ u64 weight_or_0(float x, int bin) const { return bin < kZeroBin ? weight_units(s, x) : 0; }
 
     __device__ __forceinline__ void block_min_max(u64& a, u64& b) {
         a = warp_min(a), b = warp_max(b);
@@ -460,10 +558,7 @@ private:
                 for (int j = 0; j < 8; ++j) in |= (uint32_t)(bin_of(s, x[j]) <= last) << j;
                 for (; in; in &= in - 1) {
                     const int j = __ffs(in) - 1;
-                    float v = x[0];
-#pragma unroll
-                    for (int e = 1; e < 8; ++e) v = j == e ? x[e] : v;
-                    put((u64)order_of(v) << 32 | (uint32_t)(i + j));
+                    put((u64)order_of(pick(x, j)) << 32 | (uint32_t)(i + j));
                 }
             });
         });
@@ -476,7 +571,7 @@ private:
             const float x = value_of((uint32_t)(list[i] >> 32));
             const int part = part_of(s, x, -0.5f, per_part, 256);
             atomicAdd(&sh.sub_c[part], 1u);
-            atomicAdd(&sh.sub_w[part], weight_units(s, sh.tab, x));
+            atomicAdd(&sh.sub_w[part], weight_units(s, x));
         }
         __syncthreads();
         if (warp == 0) {
@@ -543,23 +638,23 @@ private:
                 for (int k = 0; k < n_ranks; ++k) least = min(least, in[k][64]), most = max(most, in[k][65]);
                 shift = max(0, 64 - kBinBits - __clzll((long long)(most - least)));   // half of the parts are used at least
             }
-            u64* column = reinterpret_cast<u64*>(hist) + tid;
+            const uint32_t column = tc::s2u(hist) + tid * 8;
 #pragma unroll
-            for (int b = 0; b < kBins; ++b) column[b * kThreads] = 0;
+            for (int b = 0; b < kBins; ++b) sts64(column + b * (kThreads * 8), 0);
             const float z0 = bin - 0.5f;
             if (by_depth) {
                 each8([&](const float(&x)[8], int) {
                     u64 w[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) w[j] = weight_units(s, sh.tab, fmaxf(x[j], s.low));
+                    for (int j = 0; j < 8; ++j) w[j] = weight_units(s, fmaxf(x[j], s.low));
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
                         if (bin_of(s, x[j]) == bin && x[j] > -INFINITY)
-                            column[part_of(s, x[j], z0, kBins, kBins) * kThreads] += (bin < kZeroBin ? w[j] : 0) + (1ull << kWeightBits);
+                            bump(column, part_of(s, x[j], z0, kBins, kBins), (bin < kZeroBin ? w[j] : 0) + (1ull << kWeightBits));
                 });
             } else {
                 each_of(r, [&](float x, u64 o) {
-                    column[(int)((o - least) >> shift) * kThreads] += weight_or_0(x, bin) + (1ull << kWeightBits);
+                    bump(column, (int)((o - least) >> shift), weight_or_0(x, bin) + (1ull << kWeightBits));
                 });
             }
             reduce_bins();
@@ -685,7 +780,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a, in
     __syncthreads();
     const int n_ranks = cluster.num_blocks(), r = blockIdx.x / n_ranks;
     const int begin = min((int)cluster.block_rank() * segment, a.vocab), end = min(begin + segment, a.vocab);
-    RowSampler<T, kResident> row(sh, hist, reinterpret_cast<T*>(hist + HIST_BYTES), static_cast<const T*>(a.logits) + r * a.row_stride, begin, end);
+    RowSampler<T, kResident> row(sh, hist, tc::s2u(hist + HIST_BYTES), static_cast<const T*>(a.logits) + r * a.row_stride, begin, end);
     row.run(a, r);
     cluster.sync();   // no CTA leaves while another may still write into its shared memory
 }
