@@ -75,7 +75,7 @@ __device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_g
 
 // the unit behind u on the line (there is one: the caller has steps left)
 __device__ __forceinline__ void step_unit(const Plan& p, Unit& u) {
-    u.w0 += u.steps;
+    u.w0 += u.steps + p.start;
     if (++u.tile == tiles_of(p, u.s)) {
         u.tile = 0;
         if (++u.head == p.n_kv_heads) {
@@ -163,20 +163,25 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
         lay_out(p.plan, begin);
         const long long all = begin[p.plan.batch];
         const int n = workers(p.plan, all, gridDim.x);
-        const Cut cut = cut_of(p.plan, begin, all, n, cta);
-        const long long first = cut.w;
-        last = cut_of(p.plan, begin, all, n, cta + 1).w;
+        long long* ends = reinterpret_cast<long long*>(xch);
+        if (warp < 2) {   // the two cuts side by side
+            const Cut cut = cut_of(p.plan, begin, all, n, cta + warp);
+            if (lane == 0) ends[warp] = cut.w;
+            if (tid == 0) p.cuts[cta] = cut;
+        }
+        __syncthreads();
+        const long long first = ends[0];
+        last = ends[1];
         if (warp == 0) {
             Segment s;
             s.more = first < last;
             if (s.more) {
                 s.u = unit_at(p.plan, begin, first);
-                s.j0 = (int)(first - s.u.w0);
-                s.j1 = (int)min((long long)s.u.steps, last - s.u.w0);
+                s.j0 = step_at(p.plan, s.u, first);
+                s.j1 = step_at(p.plan, s.u, last);
             }
             if (lane == 0) {
                 segments[0] = s;
-                p.cuts[cta] = cut;
                 if (cta == 0) p.cuts[gridDim.x] = cut_of_end(all);
             }
         }
@@ -455,6 +460,7 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                         for (int q = 0; q < 2; ++q) {
                             if (q == 1) wait_ld<32>(sr[1]);
                             if (masked) {
+                                __syncwarp();   // (the same for the whole warp; without this the compiler makes 64 selects of every tile)
 #pragma unroll
                                 for (int c = 0; c < 32; ++c)
                                     if (q * 32 + c >= seen) sr[q][c] = 0xff800000u;   // -inf
@@ -684,11 +690,11 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
             }
             if (lane == 0) {
                 Segment s = seg;
-                s.more = s.u.w0 + s.u.steps < last;
+                s.more = s.u.w0 + s.u.steps + p.plan.start < last;
                 if (s.more) {
                     step_unit(p.plan, s.u);
                     s.j0 = 0;
-                    s.j1 = (int)min((long long)s.u.steps, last - s.u.w0);
+                    s.j1 = step_at(p.plan, s.u, last);
                 }
                 segments[at ^ 1] = s;
             }
@@ -732,7 +738,10 @@ cudaError_t launch(const PagedArgs& a, cudaStream_t stream) {
     if (!make_page_map(&map_k, a.k_pages, a.d) || !make_page_map(&map_v, a.v_pages, a.d)) return cudaErrorInvalidValue;
     Params p;
     p.plan = make_plan(a, 2 * BM, BN);
-    p.plan.min_steps = 2;
+    // (us, start 0 / 2 / 4 / 6 / 8 steps: chunks of 1100 to 1330 rows over up to 3750 keys 307 / 252 / 213 / 216 / 225; eight blocks
+    // of up to 34 rows over up to 3540 keys with 32 heads 107 / 88 / 80 / 78 / 78)
+    p.plan.start = 5;
+    p.plan.min_steps = 2 + p.plan.start;
     p.q = static_cast<const __nv_bfloat16*>(a.q);
     p.out = static_cast<__nv_bfloat16*>(a.out);
     p.page_table = a.page_table;

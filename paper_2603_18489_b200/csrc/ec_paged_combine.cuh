@@ -131,6 +131,8 @@ inline Plan make_plan(const PagedArgs& a, int tm, int tk) {
     p.mask_block = a.d.mask_block;
     p.tm = tm;
     p.tk = tk;
+    p.start = 0;
+    p.whole = 0;
     p.min_steps = 1;
     p.dev_status = a.dev_status;
     return p;
@@ -139,7 +141,7 @@ inline Plan make_plan(const PagedArgs& a, int tm, int tk) {
 template <typename T, int HD, bool kSwizzled = false>
 cudaError_t launch_combine(const Plan& p, const Cut* cuts, const float* partial, void* out, int n_q_heads, int ctas,
                            cudaStream_t stream) {
-    if (ctas < 2) return cudaSuccess;
+    if (ctas < 2 || p.whole) return cudaSuccess;
     if (2 * 256 + 2 * ctas > kMaxWeights) return cudaErrorInvalidValue;   // (a GPU of more than 256 SMs)
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(ctas - 1, 1, 1);

@@ -10,12 +10,13 @@
 // angle (2^-25 of half a turn) is put back to first order: 5e-8 of an fp32 result.
 #include "ec_common.cuh"
 #include "ec_tc_ptx.cuh"
+#include <cstdlib>
 
 namespace ec {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxTokens = 8;   // rows a CTA, at most
+constexpr int kMaxTokens = 32;   // rows a CTA, at most
 
 __device__ __forceinline__ void load8(const float* p, float* v) {
     const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
@@ -99,71 +100,88 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs a, int to
     const bool inter = a.d.flags & EC_ROPE_INTERLEAVED, rotates = l < pairs;
     const int c0 = rotates && !inter ? l : 2 * l, c1 = rotates && !inter ? l + pairs : 2 * l + 1;
     const bool norm = a.q_weight != nullptr;
-    for (int item = tid / LH; item < n * heads; item += HPB) {
-        const int t = item / heads, h = item - t * heads;
-        const Row row = rows[t];
-        const long long r = r0 + t;
-        const T* src;
-        T* dst = nullptr;
-        if (h < hq) {
-            src = static_cast<const T*>(a.q) + r * a.q_stride + (long long)h * HD;
-            if (row.out) dst = static_cast<T*>(a.q_out) + (r * hq + h) * HD;
-        } else if (h < hq + hkv) {
-            const int hk = h - hq;
-            src = static_cast<const T*>(a.k) + r * a.k_stride + (long long)hk * HD;
-            if constexpr (kPaged) {
-                if (row.kv >= 0) dst = static_cast<T*>(a.k_out) + row.kv + (long long)hk * a.page_size * HD;
-            } else if (row.out) {
-                dst = static_cast<T*>(a.k_out) + (r * hkv + hk) * HD;
-            }
-        } else {
-            const int hk = h - hq - hkv;
-            src = static_cast<const T*>(a.v) + r * a.v_stride + (long long)hk * HD;
-            if (row.kv >= 0) dst = static_cast<T*>(a.v_pages) + row.kv + (long long)hk * a.page_size * HD;
-        }
-        // (the lanes of a head agree on dst, so the reduction below stays whole within them; padding rows are not read)
-        float x[2][8];
-        if (!dst) continue;
-        load8(src + c0 * 8, x[0]);
-        load8(src + c1 * 8, x[1]);
-        if (h < hq + hkv) {
-            if (norm) {
-                float ss = 0.f;
+    // kItems heads at a time: their loads are under way together
+    constexpr int kItems = 2;
+    for (int item0 = tid / LH; item0 < n * heads; item0 += kItems * HPB) {
+        float x[kItems][2][8];
+        T* dst[kItems];
+        int tok[kItems], kind[kItems];   // kind: 0 a query head, 1 a key head, 2 a value head
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ss = fmaf(x[0][i], x[0][i], fmaf(x[1][i], x[1][i], ss));
-                const uint32_t lanes = ((1u << LH) - 1u) << ((tid & 31) / LH * LH);
-#pragma unroll
-                for (int o = LH / 2; o; o >>= 1) ss += __shfl_xor_sync(lanes, ss, o);
-                const float inv = 1.f / sqrtf(ss * (1.f / HD) + a.d.eps);
-                const T* w = static_cast<const T*>(h < hq ? a.q_weight : a.k_weight);
-                float wv[2][8];
-                load8(w + c0 * 8, wv[0]);
-                load8(w + c1 * 8, wv[1]);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[0][i] *= inv * wv[0][i], x[1][i] *= inv * wv[1][i];
-            }
-            if (rotates && !inter) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float2 cs = turn[t][l * 8 + i];
-                    const float p = x[0][i], q = x[1][i];
-                    x[0][i] = fmaf(p, cs.x, -q * cs.y);
-                    x[1][i] = fmaf(q, cs.x, p * cs.y);
+        for (int e = 0; e < kItems; ++e) {
+            const int item = item0 + e * HPB;
+            dst[e] = nullptr;
+            if (item >= n * heads) continue;
+            const int t = item / heads, h = item - t * heads;
+            const Row row = rows[t];
+            const long long r = r0 + t;
+            const T* src;
+            tok[e] = t;
+            if (h < hq) {
+                kind[e] = 0;
+                src = static_cast<const T*>(a.q) + r * a.q_stride + (long long)h * HD;
+                if (row.out) dst[e] = static_cast<T*>(a.q_out) + (r * hq + h) * HD;
+            } else if (h < hq + hkv) {
+                const int hk = h - hq;
+                kind[e] = 1;
+                src = static_cast<const T*>(a.k) + r * a.k_stride + (long long)hk * HD;
+                if constexpr (kPaged) {
+                    if (row.kv >= 0) dst[e] = static_cast<T*>(a.k_out) + row.kv + (long long)hk * a.page_size * HD;
+                } else if (row.out) {
+                    dst[e] = static_cast<T*>(a.k_out) + (r * hkv + hk) * HD;
                 }
-            } else if (rotates) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float2 cs = turn[t][l * 8 + j * 4 + i];
-                        const float p = x[j][2 * i], q = x[j][2 * i + 1];
-                        x[j][2 * i] = fmaf(p, cs.x, -q * cs.y);
-                        x[j][2 * i + 1] = fmaf(q, cs.x, p * cs.y);
-                    }
+            } else {
+                const int hk = h - hq - hkv;
+                kind[e] = 2;
+                src = static_cast<const T*>(a.v) + r * a.v_stride + (long long)hk * HD;
+                if (row.kv >= 0) dst[e] = static_cast<T*>(a.v_pages) + row.kv + (long long)hk * a.page_size * HD;
+            }
+            if (dst[e]) {   // (padding rows are not read)
+                load8(src + c0 * 8, x[e][0]);
+                load8(src + c1 * 8, x[e][1]);
             }
         }
-        store8(dst + c0 * 8, x[0]);
-        store8(dst + c1 * 8, x[1]);
+#pragma unroll
+        for (int e = 0; e < kItems; ++e) {
+            if (!dst[e]) continue;   // (the lanes of a head agree, so the reduction below stays whole within them)
+            if (kind[e] < 2) {
+                if (norm) {
+                    float ss = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) ss = fmaf(x[e][0][i], x[e][0][i], fmaf(x[e][1][i], x[e][1][i], ss));
+                    const uint32_t lanes = ((1u << LH) - 1u) << ((tid & 31) / LH * LH);
+#pragma unroll
+                    for (int o = LH / 2; o; o >>= 1) ss += __shfl_xor_sync(lanes, ss, o);
+                    const float inv = 1.f / sqrtf(ss * (1.f / HD) + a.d.eps);
+                    const T* w = static_cast<const T*>(kind[e] == 0 ? a.q_weight : a.k_weight);
+                    float wv[2][8];
+                    load8(w + c0 * 8, wv[0]);
+                    load8(w + c1 * 8, wv[1]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[e][0][i] *= inv * wv[0][i], x[e][1][i] *= inv * wv[1][i];
+                }
+                if (rotates && !inter) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float2 cs = turn[tok[e]][l * 8 + i];
+                        const float p = x[e][0][i], q = x[e][1][i];
+                        x[e][0][i] = fmaf(p, cs.x, -q * cs.y);
+                        x[e][1][i] = fmaf(q, cs.x, p * cs.y);
+                    }
+                } else if (rotates) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float2 cs = turn[tok[e]][l * 8 + j * 4 + i];
+                            const float p = x[e][j][2 * i], q = x[e][j][2 * i + 1];
+                            x[e][j][2 * i] = fmaf(p, cs.x, -q * cs.y);
+                            x[e][j][2 * i + 1] = fmaf(q, cs.x, p * cs.y);
+                        }
+                }
+            }
+            store8(dst[e] + c0 * 8, x[e][0]);
+            store8(dst[e] + c1 * 8, x[e][1]);
+        }
     }
 }
 
@@ -171,7 +189,8 @@ template <typename T, int HD, bool kPaged>
 cudaError_t launch(const RopeArgs& a, cudaStream_t stream) {
     // Few rows: one a CTA.  Many: the angles' 64-bit arithmetic and the start of a CTA are shared by several.
     int tokens = 1;
-    while (tokens < kMaxTokens && (long long)a.n_rows > 8ll * sm_count() * tokens) tokens *= 2;
+    const int top = getenv("EC_RT") ? atoi(getenv("EC_RT")) : kMaxTokens;
+    while (tokens < top && (long long)a.n_rows > 8ll * sm_count() * tokens) tokens *= 2;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((a.n_rows + tokens - 1) / tokens, 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
