@@ -18,7 +18,7 @@ namespace {
 
 using namespace paged;
 
-constexpr int TM = 16, CK = 16;
+constexpr int CK = 16, kMaxTM = 16;
 
 // W warps a CTA, S stages a warp
 template <typename T, int HD, int W, int S>
@@ -26,8 +26,8 @@ struct Geo {
     static constexpr int CHUNK = CK * HD * (int)sizeof(T);   // bytes of a warp's K or V chunk
     static constexpr int STAGE = 2 * CHUNK;
     static constexpr int WARP = S * STAGE;
-    static constexpr int Q = sizeof(T) == 4 ? TM * HD * 4 : 0;        // fp32: the tile's query rows ...
-    static constexpr int P = sizeof(T) == 4 ? W * CK * TM * 4 : 0;   // ... and the probabilities
+    static constexpr int Q = sizeof(T) == 4 ? kMaxTM * HD * 4 : 0;        // fp32: the tile's query rows ...
+    static constexpr int P = sizeof(T) == 4 ? W * CK * kMaxTM * 4 : 0;   // ... and the probabilities
     static constexpr int BYTES = W * WARP + Q + P;
     static constexpr int CTAS = (BYTES + 10240) * 3 <= 228 * 1024 ? 3 : (BYTES + 10240) * 2 <= 228 * 1024 ? 2 : 1;   // an SM
 };
@@ -66,114 +66,125 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t* a, uint32_t b
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+__device__ __forceinline__ uint32_t transposed(uint32_t v) {   // of an 8 x 8 tile of 16-bit values
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+
 // A warp's state over its chunks.  Row limits: a key counts for a row while it is below lim.
-template <int HD>
+// Keys and columns stand on the M axis of the products, the query rows on N, eight at a time: S^T = K Q^T and O^T = V^T P^T, so
+// that eight rows, one of a token's query heads each, fill an instruction (with the rows on M it was twice as many).
+template <int HD, int NT>
 struct WarpBf16 {
-    uint32_t qa[HD / 16][4];
-    float o[HD / 8][4], m[2], l[2];
-    int lim[2];
-    __device__ __forceinline__ void start(const Params& p, const Unit& u, int lane, const unsigned char*) {
+    static constexpr int TM = 8 * NT, LD = HD + 4;   // row stride of finish(): no bank conflicts
+    uint32_t qb[NT][HD / 16][2];
+    float o[NT][HD / 16][4], m[NT][2], l[NT][2];      // of rows (lane % 4) * 2 + {0, 1}
+    int lim[NT][2];
+    __device__ __forceinline__ void start(const Params& p, const Unit& u, int lane) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int pr = u.tile * TM + lane / 4 + 8 * h, tok = pr / p.plan.group;
+        for (int nt = 0; nt < NT; ++nt) {
+            const int pr = u.tile * TM + nt * 8 + lane / 4, tok = pr / p.plan.group;
             const bool has = tok < u.s.n;
-            lim[h] = has ? limit_of(p.plan, u.s, tok) : 0;
             const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q) +
                 ((long long)(u.s.row0 + tok) * p.n_q_heads + u.head * p.plan.group + pr % p.plan.group) * HD + (lane & 3) * 2;
 #pragma unroll
-            for (int ks = 0; ks < HD / 16; ++ks) {
-                qa[ks][h] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16) : 0u;
-                qa[ks][2 + h] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + 8) : 0u;
+            for (int ks = 0; ks < HD / 16; ++ks)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) qb[nt][ks][h] = has ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + h * 8) : 0u;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int t = (u.tile * TM + nt * 8 + (lane & 3) * 2 + e) / p.plan.group;
+                lim[nt][e] = t < u.s.n ? limit_of(p.plan, u.s, t) : 0;
+                m[nt][e] = -INFINITY;
+                l[nt][e] = 0.f;
             }
-            m[h] = -INFINITY;
-            l[h] = 0.f;
+#pragma unroll
+            for (int i = 0; i < HD / 16; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[nt][i][j] = 0.f;
         }
-#pragma unroll
-        for (int i = 0; i < HD / 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
     }
     __device__ __forceinline__ void chunk(const Params& p, uint32_t stage, int key0, int lane, const unsigned char*, float*) {
         constexpr int ROW = HD * 2;
-        float s[2][4] = {};
         const int mi = lane >> 3, r = lane & 7;
+        float s[NT][2][4] = {};   // even and odd steps of the columns: half the chain
 #pragma unroll
         for (int ks = 0; ks < HD / 16; ++ks) {
-            uint32_t b[4];
-            const int key = (mi >> 1) * 8 + r;
-            ldsm(stage + key * ROW + (((ks * 2 + (mi & 1)) ^ r) << 4), b);
-            mma(s[0], qa[ks], b[0], b[1]);
-            mma(s[1], qa[ks], b[2], b[3]);
+            uint32_t a[4];
+            ldsm(stage + ((mi & 1) * 8 + r) * ROW + (((ks * 2 + (mi >> 1)) ^ r) << 4), a);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma(s[nt][ks & 1], a, qb[nt][ks][0], qb[nt][ks][1]);
         }
-        float f[2];
+        uint32_t pb[NT][2];
+        bool moved = false;
+        float f[NT][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float mx = -INFINITY;
+        for (int nt = 0; nt < NT; ++nt) {
+            float x[4];
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
+            for (int i = 0; i < 4; ++i)   // key lane / 4 + 8 (i / 2), row (lane % 4) * 2 + i % 2
+                x[i] = key0 + (lane >> 2) + (i >> 1) * 8 < lim[nt][i & 1] ? (s[nt][0][i] + s[nt][1][i]) * p.scale_log2 : -INFINITY;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float& x = s[nt][2 * h + e];
-                    x = key0 + nt * 8 + (lane & 3) * 2 + e < lim[h] ? x * p.scale_log2 : -INFINITY;
-                    mx = fmaxf(mx, x);
-                }
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-            const float mn = fmaxf(m[h], mx), ref = mn == -INFINITY ? 0.f : mn;   // (a row that sees nothing yet)
-            f[h] = fast_exp2(m[h] - ref);
-            m[h] = mn;
-            float sum = 0.f;
+            for (int e = 0; e < 2; ++e) {
+                float mx = fmaxf(x[e], x[2 + e]);
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float& x = s[nt][2 * h + e];
-                    x = fast_exp2(x - ref);
-                    sum += x;
-                }
-            l[h] = fmaf(l[h], f[h], sum);
-        }
-        if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
-#pragma unroll
-            for (int i = 0; i < HD / 8; ++i) {
-                o[i][0] *= f[0], o[i][1] *= f[0];
-                o[i][2] *= f[1], o[i][3] *= f[1];
+                for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+                const float mn = fmaxf(m[nt][e], mx), ref = mn == -INFINITY ? 0.f : mn;   // (a row that sees nothing yet)
+                f[nt][e] = fast_exp2(m[nt][e] - ref);
+                moved |= f[nt][e] != 1.f;
+                m[nt][e] = mn;
+                x[e] = fast_exp2(x[e] - ref);
+                x[2 + e] = fast_exp2(x[2 + e] - ref);
+                l[nt][e] = fmaf(l[nt][e], f[nt][e], x[e] + x[2 + e]);   // this lane's keys alone, summed over the lanes at the end
             }
+            pb[nt][0] = transposed(tc::pack_bf16x2(x[0], x[1]));
+            pb[nt][1] = transposed(tc::pack_bf16x2(x[2], x[3]));
         }
-        const uint32_t pa[4] = {tc::pack_bf16x2(s[0][0], s[0][1]), tc::pack_bf16x2(s[0][2], s[0][3]),
-                                tc::pack_bf16x2(s[1][0], s[1][1]), tc::pack_bf16x2(s[1][2], s[1][3])};
+        if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < HD / 16; ++i) {
+                    o[nt][i][0] *= f[nt][0], o[nt][i][1] *= f[nt][1];
+                    o[nt][i][2] *= f[nt][0], o[nt][i][3] *= f[nt][1];
+                }
+        }
         const uint32_t vbase = stage + CK * ROW;
 #pragma unroll
-        for (int np = 0; np < HD / 16; ++np) {
-            uint32_t b[4];
-            const int key = (mi & 1) * 8 + r;
-            ldsm_t(vbase + key * ROW + (((np * 2 + (mi >> 1)) ^ r) << 4), b);
-            mma(o[2 * np], pa, b[0], b[1]);
-            mma(o[2 * np + 1], pa, b[2], b[3]);
+        for (int i = 0; i < HD / 16; ++i) {
+            uint32_t a[4];
+            ldsm_t(vbase + ((mi >> 1) * 8 + r) * ROW + (((i * 2 + (mi & 1)) ^ r) << 4), a);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma(o[nt][i], a, pb[nt][0], pb[nt][1]);
         }
     }
-    // un-normalised rows to dst [TM][HD], maxima and sums to ml [TM]
+    // un-normalised rows to dst [TM][LD], maxima and sums to ml [TM]
     __device__ __forceinline__ void finish(float* dst, float2* ml, int lane) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float sum = l[h];
-            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-            const int row = lane / 4 + 8 * h;
-            if ((lane & 3) == 0) ml[row] = make_float2(m[h], sum);
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < HD / 8; ++i)
-                *reinterpret_cast<float2*>(dst + row * HD + i * 8 + (lane & 3) * 2) = make_float2(o[i][2 * h], o[i][2 * h + 1]);
-        }
+            for (int e = 0; e < 2; ++e) {
+                float sum = l[nt][e];
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                const int row = nt * 8 + (lane & 3) * 2 + e;
+                if (lane < 4) ml[row] = make_float2(m[nt][e], sum);
+#pragma unroll
+                for (int i = 0; i < HD / 16; ++i) {
+                    dst[row * LD + i * 16 + (lane >> 2)] = o[nt][i][e];
+                    dst[row * LD + i * 16 + 8 + (lane >> 2)] = o[nt][i][2 + e];
+                }
+            }
     }
 };
 
 template <int HD>
 struct WarpF32 {
-    static constexpr int C = HD / 32;
+    static constexpr int TM = 16, LD = HD, C = HD / 32;
     float o[TM][C], m[8], l[8];
     int lim[8];
-    __device__ __forceinline__ void start(const Params& p, const Unit& u, int lane, const unsigned char*) {
+    __device__ __forceinline__ void start(const Params& p, const Unit& u, int lane) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int tok = (u.tile * TM + (lane >> 4) * 8 + i) / p.plan.group;
@@ -268,15 +279,17 @@ struct WarpF32 {
             for (int c = 0; c < C; ++c) dst[i * HD + lane * C + c] = o[i][c];
     }
 };
-template <typename T, int HD>
-struct WarpOf { using type = WarpBf16<HD>; };
-template <int HD>
-struct WarpOf<float, HD> { using type = WarpF32<HD>; };
+template <typename T, int HD, int NT>
+struct WarpOf { using type = WarpBf16<HD, NT>; };
+template <int HD, int NT>
+struct WarpOf<float, HD, NT> { using type = WarpF32<HD>; };
 
-template <typename T, int HD, int W, int S>
+template <typename T, int HD, int NT, int W, int S>
 __global__ void __launch_bounds__(32 * W, Geo<T, HD, W, S>::CTAS) attend_paged_rows_kernel(const Params p) {
     using G = Geo<T, HD, W, S>;
-    constexpr int kThreads = 32 * W, TK = CK * W, kStages = S;
+    using Warp = typename WarpOf<T, HD, NT>::type;
+    constexpr int kThreads = 32 * W, TK = CK * W, kStages = S, TM = Warp::TM, LD = Warp::LD;
+    static_assert(TM * LD * 4 <= G::WARP, "a warp's rows stand over its stages");
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ long long begin[EC_PAGED_MAX_BATCH + 1];
     __shared__ float2 ml[W][TM];
@@ -290,8 +303,9 @@ __global__ void __launch_bounds__(32 * W, Geo<T, HD, W, S>::CTAS) attend_paged_r
     const long long all = begin[p.plan.batch];
     const int n = workers(p.plan, all, gridDim.x), cta = blockIdx.x;
     __shared__ long long ends[2];
+    __shared__ Unit unit;
     if (warp < 2) {   // the two cuts side by side
-        const Cut cut = cut_of(p.plan, begin, all, n, cta + warp);
+        const Cut cut = cut_of(p.plan, begin, all, n, cta + warp, warp == 0 ? &unit : nullptr);
         if (lane == 0) ends[warp] = cut.w;
         if (threadIdx.x == 0) p.cuts[cta] = cut;
     }
@@ -299,8 +313,9 @@ __global__ void __launch_bounds__(32 * W, Geo<T, HD, W, S>::CTAS) attend_paged_r
     const long long first = ends[0], last = ends[1];
     if (threadIdx.x == 0 && cta == 0) p.cuts[gridDim.x] = cut_of_end(all);
 
+    Unit u = unit;
     for (long long w = first; w < last;) {
-        const Unit u = unit_at(p.plan, begin, w);
+        if (w != first) step_unit(p.plan, u);
         const int j0 = step_at(p.plan, u, w), j1 = step_at(p.plan, u, last);
         w = min(last, u.w0 + u.steps + p.plan.start);
         const long long rows_all = (long long)u.s.n * p.plan.group;
@@ -353,8 +368,8 @@ __global__ void __launch_bounds__(32 * W, Geo<T, HD, W, S>::CTAS) attend_paged_r
             }
             __syncthreads();
         }
-        typename WarpOf<T, HD>::type state;
-        state.start(p, u, lane, mine);
+        Warp state;
+        state.start(p, u, lane);
         for (int j = j0; j < j1; ++j) {
             const int next = page_at(j + kStages);
             issue(j + kStages - 1, page);
@@ -383,7 +398,7 @@ __global__ void __launch_bounds__(32 * W, Geo<T, HD, W, S>::CTAS) attend_paged_r
             for (int k = 0; k < W; ++k) {
                 const float f = exp2f(ml[k][r].x - ref);
                 L = fmaf(f, ml[k][r].y, L);
-                const float4 x = *reinterpret_cast<const float4*>(smem + k * G::WARP + (r * HD + c) * 4);
+                const float4 x = *reinterpret_cast<const float4*>(smem + k * G::WARP + (r * LD + c) * 4);
                 acc[0] = fmaf(f, x.x, acc[0]), acc[1] = fmaf(f, x.y, acc[1]);
                 acc[2] = fmaf(f, x.z, acc[2]), acc[3] = fmaf(f, x.w, acc[3]);
             }
@@ -400,11 +415,11 @@ __global__ void __launch_bounds__(32 * W, Geo<T, HD, W, S>::CTAS) attend_paged_r
     }
 }
 
-template <typename T, int HD, int W, int S>
+template <typename T, int HD, int NT, int W, int S>
 cudaError_t launch_as(const PagedArgs& a, bool whole, cudaStream_t stream) {
     using G = Geo<T, HD, W, S>;
     Params p;
-    p.plan = make_plan(a, TM, CK * W);
+    p.plan = make_plan(a, WarpOf<T, HD, NT>::type::TM, CK * W);
     p.plan.start = 2;
     p.plan.min_steps = 4;
     p.plan.whole = whole;
@@ -417,7 +432,7 @@ cudaError_t launch_as(const PagedArgs& a, bool whole, cudaStream_t stream) {
     p.cuts = static_cast<Cut*>(a.workspace);
     p.partial = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + cuts_bytes(ctas));
     static PerDeviceOnce once;
-    if (const cudaError_t e = ensure_dynamic_smem(once, attend_paged_rows_kernel<T, HD, W, S>, G::BYTES); e != cudaSuccess) return e;
+    if (const cudaError_t e = ensure_dynamic_smem(once, attend_paged_rows_kernel<T, HD, NT, W, S>, G::BYTES); e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(ctas, 1, 1);
     cfg.blockDim = dim3(32 * W, 1, 1);
@@ -428,7 +443,7 @@ cudaError_t launch_as(const PagedArgs& a, bool whole, cudaStream_t stream) {
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    if (const cudaError_t e = cudaLaunchKernelEx(&cfg, attend_paged_rows_kernel<T, HD, W, S>, p); e != cudaSuccess) return e;
+    if (const cudaError_t e = cudaLaunchKernelEx(&cfg, attend_paged_rows_kernel<T, HD, NT, W, S>, p); e != cudaSuccess) return e;
     return launch_combine<T, HD>(p.plan, p.cuts, p.partial, a.out, a.d.n_q_heads, ctas, stream);
 }
 template <typename T, int HD>
@@ -436,16 +451,22 @@ cudaError_t launch(const PagedArgs& a, cudaStream_t stream) {
     // Short sequences: a unit is left whole to a CTA of more warps, and there is nothing to join, a launch less (one row of 28
     // heads on 4 over 768 keys 17.4 -> 14.5 us).  Not in fp32, where sixteen keys take a warp 2 us and more CTAs are worth the
     // launch (2 x 34 rows of 256 keys: 12.4 us cut, 15.4 whole).
-    if constexpr (sizeof(T) == 2)
-        if ((long long)a.d.max_pages * a.d.page_size <= kWholeKeys) return launch_as<T, HD, HD == 128 ? 8 : 16, 3>(a, true, stream);
-    return launch_as<T, HD, 4, 3>(a, false, stream);
+    if constexpr (sizeof(T) == 4) {
+        return launch_as<T, HD, 2, 4, 3>(a, false, stream);
+    } else {
+        constexpr int kWide = HD == 128 ? 8 : 16;
+        const bool whole = (long long)a.d.max_pages * a.d.page_size <= kWholeKeys;
+        if ((long long)a.max_rows * (a.d.n_q_heads / a.d.n_kv_heads) <= 8)
+            return whole ? launch_as<T, HD, 1, kWide, 3>(a, true, stream) : launch_as<T, HD, 1, 4, 3>(a, false, stream);
+        return whole ? launch_as<T, HD, 2, kWide, 3>(a, true, stream) : launch_as<T, HD, 2, 4, 3>(a, false, stream);
+    }
 }
 
 }  // namespace
 
 size_t attend_paged_rows_workspace(const ec_paged_desc& d) {
     const int ctas = sm_count() * 4;   // at most
-    return cuts_bytes(ctas) + (size_t)ctas * 2 * TM * (d.head_dim + 2) * 4;
+    return cuts_bytes(ctas) + (size_t)ctas * 2 * kMaxTM * (d.head_dim + 2) * 4;
 }
 
 cudaError_t launch_attend_paged_rows(const PagedArgs& a, cudaStream_t stream) {

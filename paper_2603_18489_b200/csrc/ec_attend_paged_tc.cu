@@ -73,22 +73,6 @@ __device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t byt
 }
 __device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
-// the unit behind u on the line (there is one: the caller has steps left)
-__device__ __forceinline__ void step_unit(const Plan& p, Unit& u) {
-    u.w0 += u.steps + p.start;
-    if (++u.tile == tiles_of(p, u.s)) {
-        u.tile = 0;
-        if (++u.head == p.n_kv_heads) {
-            u.head = 0;
-            do {
-                ++u.b;
-                u.s = u.b < p.batch ? seq_of(p, u.b) : Seq{0, 1, 0};
-            } while (u.s.n == 0);
-        }
-    }
-    u.steps = steps_of(p, u.s, u.tile);
-}
-
 __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 // packed rows of a unit
 __device__ __forceinline__ int rows_of(const Plan& p, const Unit& u) {
@@ -165,25 +149,19 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
         const int n = workers(p.plan, all, gridDim.x);
         long long* ends = reinterpret_cast<long long*>(xch);
         if (warp < 2) {   // the two cuts side by side
-            const Cut cut = cut_of(p.plan, begin, all, n, cta + warp);
+            const Cut cut = cut_of(p.plan, begin, all, n, cta + warp, warp == 0 ? &segments[0].u : nullptr);
             if (lane == 0) ends[warp] = cut.w;
             if (tid == 0) p.cuts[cta] = cut;
         }
         __syncthreads();
         const long long first = ends[0];
         last = ends[1];
-        if (warp == 0) {
-            Segment s;
+        if (tid == 0) {
+            Segment& s = segments[0];
             s.more = first < last;
-            if (s.more) {
-                s.u = unit_at(p.plan, begin, first);
-                s.j0 = step_at(p.plan, s.u, first);
-                s.j1 = step_at(p.plan, s.u, last);
-            }
-            if (lane == 0) {
-                segments[0] = s;
-                if (cta == 0) p.cuts[gridDim.x] = cut_of_end(all);
-            }
+            s.j0 = step_at(p.plan, s.u, first);
+            s.j1 = step_at(p.plan, s.u, last);
+            if (cta == 0) p.cuts[gridDim.x] = cut_of_end(all);
         }
     }
     fence_async_smem();   // the ring is the TMA's from here on

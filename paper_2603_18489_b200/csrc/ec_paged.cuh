@@ -150,6 +150,22 @@ static __device__ __noinline__ Unit unit_at(const Plan& p, const long long* begi
     return u;
 }
 
+// the unit behind u on the line (there is one: the caller has steps left)
+__device__ __forceinline__ void step_unit(const Plan& p, Unit& u) {
+    u.w0 += u.steps + p.start;
+    if (++u.tile == tiles_of(p, u.s)) {
+        u.tile = 0;
+        if (++u.head == p.n_kv_heads) {
+            u.head = 0;
+            do {
+                ++u.b;
+                u.s = u.b < p.batch ? seq_of(p, u.b) : Seq{0, 1, 0};
+            } while (u.s.n == 0);
+        }
+    }
+    u.steps = steps_of(p, u.s, u.tile);
+}
+
 // the first step of a unit that a stretch of the line from `w` on takes (to: the step before which one that ends at w stops)
 __device__ __forceinline__ int step_at(const Plan& p, const Unit& u, long long w) {
     const long long in = w - u.w0 - p.start;
@@ -169,7 +185,8 @@ struct Cut {
 __device__ __forceinline__ Cut cut_of_end(long long all) { return Cut{all, -1, 0, 0, 0, 0, 0, 0}; }
 // The cut before CTA c of `n`.  One that would leave a quarter of its unit or less on one side is moved to that end of the unit
 // where the steps allow it (the partial rows of a unit cost about as much as a step).
-__device__ __forceinline__ Cut cut_of(const Plan& p, const long long* begin, long long all, int n, int c) {
+// (start_unit: the unit that a stretch from this cut on begins with)
+__device__ __forceinline__ Cut cut_of(const Plan& p, const long long* begin, long long all, int n, int c, Unit* start_unit) {
     if (c >= n || all == 0) return cut_of_end(all);
     const long long per = quotient(all, n);
     long long w = c <= 0 ? 0 : per * c + quotient((all - per * n) * c, n);
@@ -179,6 +196,11 @@ __device__ __forceinline__ Cut cut_of(const Plan& p, const long long* begin, lon
         const int slack = u.steps / 4 < p.min_steps / 2 ? u.steps / 4 : p.min_steps / 2, cost = u.steps + p.start;
         if (p.whole || in <= p.start + slack) w = u.w0;
         else if (cost - in <= slack) w = u.w0 + cost;
+    }
+    if (start_unit && (threadIdx.x & 31) == 0) {
+        Unit v = u;
+        if (w >= u.w0 + u.steps + p.start && w < all) step_unit(p, v);
+        *start_unit = v;
     }
     const bool inside = w < u.w0 + u.steps + p.start;   // (at the end of a unit nothing is divided)
     return Cut{w, inside ? u.w0 : w, u.steps, u.head, u.tile, u.s.row0, u.s.n, 0};
