@@ -38,7 +38,7 @@ constexpr int kSegment = kThreads * 1016;  // elements of a CTA: 1016 weights of
 constexpr int kList = kThreads * kBins / 2;   // candidates that a search takes out of the row: two lists of them over the bins
 constexpr int kFew = 128;                  // candidates that are ranked against one another
 constexpr uint32_t HIST_BYTES = kBins * kThreads * 8;
-constexpr int kMaxDynamic = 232448 - 25600;   // (the rest: struct Shared)
+constexpr int kMaxDynamic = 232448 - 34816;   // (the rest: struct Shared)
 constexpr int kMaxUnitBits = 47;
 // a thread's weights, none above one, have to fit kWeightBits: as fine a unit as the whole row on one CTA leaves room for
 __host__ __device__ constexpr int unit_bits_of(int vocab) {
@@ -46,6 +46,7 @@ __host__ __device__ constexpr int unit_bits_of(int vocab) {
     while (bits > 43 && (long long)((vocab + 4095) / 4096 * 8) << bits > 1ll << kWeightBits) --bits;
     return bits;
 }
+constexpr int kFine = 1024;                // fine bins: counts alone; the last: weights that round to 0
 typedef unsigned long long u64;
 
 // 2^(i / 64), i = 0 .. 63, from its definition; a copy for each of sixteen lanes (a half warp's 8-byte loads never meet in a bank)
@@ -82,6 +83,7 @@ __device__ __forceinline__ void sts128(uint32_t at, const uint4& v) {
 struct Scale {   // what turns a logit of this row into a bin and a weight
     float top, per_bin;   // bin = (top - x) * per_bin, to the nearest
     float low;            // what is below it weighs nothing
+    float per_fine, nats;   // the same for the fine bins, and what a fine bin spans
     double wide_top, c;   // (x - top) * c = 64 log2 of the weight
     uint32_t table;       // shared address of this lane's copy of ExpTable
     double round, unit;   // 2^(52 - bits), whose last bit is one unit of weight, and 2^bits
@@ -89,6 +91,9 @@ struct Scale {   // what turns a logit of this row into a bin and a weight
 // (every step of these three is monotone in x, so what they tell apart are intervals of the order)
 __device__ __forceinline__ float depth_of(const Scale& s, float x) { return fminf((s.top - x) * s.per_bin, (float)kZeroBin); }
 __device__ __forceinline__ int bin_of(const Scale& s, float x) { return __float_as_int(depth_of(s, x) + 8388608.f) & kZeroBin; }
+__device__ __forceinline__ int fine_of(const Scale& s, float x) {
+    return __float_as_int(fminf((s.top - x) * s.per_fine, (float)(kFine - 1)) + 8388608.f) & (kFine - 1);
+}
 // part of the interval [z0, z0 + parts / per_part) of depths
 __device__ __forceinline__ int part_of(const Scale& s, float x, float z0, float per_part, int parts) {
     return min(max(__float2int_rz((depth_of(s, x) - z0) * per_part), 0), parts - 1);
@@ -141,8 +146,11 @@ struct Shared {
     u64 bin_w[kBins], bin_c[kBins], all_w, all_c, red_a[kWarps], red_b[kWarps];
     Found found;
     u64 cand_w[kFew];
-    u64 sub_w[256], part_w[256];
-    uint32_t sub_c[256], part_c[256];
+    u64 part_w[256];
+    uint32_t part_c[256];
+    uint32_t fine[kFine], cum_c[kFine];   // counts of this CTA; of the row, running
+    float cum_e[kFine];                   // running weights, estimated from the counts
+    int done;
     uint32_t n_list, n_next;
     u64 pick[4];
 };
@@ -245,30 +253,25 @@ public:
         // the other bins over the nats above half a unit, (bits + 1) ln 2 < 33.4 of them, or over the whole row where that spans less
         const float span = (s.top - value_of((uint32_t)low64)) / t;
         s.per_bin = fminf((kZeroBin - 0.55f) / fmaxf(fminf(span * 1.001f, 33.4f), 1e-30f) / t, 1e37f);   // (finite: 0 times it is 0)
-        // ---- counts and weights by bin, and of the tokens that min-p keeps ----
+        s.nats = fmaxf(fminf(span * 1.001f, 33.4f), 1e-30f) / (kFine - 1.6f);
+        s.per_fine = fminf(1.f / s.nats / t, 1e37f);
+        s.low = s.top - kZeroBin / s.per_bin;
+        const int k = a.top_k ? a.top_k[r] : 0;
+        const float p = a.top_p ? a.top_p[r] : 1.f;
+        const double u = (double)a.u[r];
         const float mp = a.min_p ? a.min_p[r] : 0.f;
         // (at least the largest stays; a bound below a unit asks the exponents instead of the weights)
         const u64 floor_units = mp > 0.f ? (u64)fmin(ceil((double)mp * s.unit), s.unit) : 0;
         const bool tiny = floor_units == 1;
         const double least_u = tiny ? 64.0 * log2((double)mp) : 0.0;
+        constexpr u64 kOne = 1ull << kWeightBits;
+        if (by_estimate(a, r, k, p, mp, u, floor_units, tiny, least_u)) return;
+
+        // ---- what the estimates could not settle: weights by bin, and searches that narrow a bin down ----
         const uint32_t column = tc::s2u(hist) + tid * 8;
 #pragma unroll
         for (int b = 0; b < kBins; ++b) sts64(column + b * (kThreads * 8), 0);
         u64 kept_c = 0, kept_w = 0;
-        s.low = s.top - kZeroBin / s.per_bin;
-        const int k = a.top_k ? a.top_k[r] : 0;
-        constexpr u64 kOne = 1ull << kWeightBits;
-        if (k > 0 && k <= kList / 2) {
-            // The first k tokens are all that counts, and (nearly always) they fit the list: their weights are formed there
-            each8([&](const float(&x)[8], int) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    bump(column, bin_of(s, x[j]), x[j] > -INFINITY ? kOne : 0);
-            });
-            if (count_bins(a, r, k)) return;
-#pragma unroll
-            for (int b = 0; b < kBins; ++b) sts64(column + b * (kThreads * 8), 0);
-        }
         // (eight weights at a time without a branch: one alone is a chain of ten 64-bit operations)
         const auto weigh = [&](auto with_floor) {
             const u64 one = kOne - (u64)__double_as_longlong(s.round);
@@ -303,25 +306,17 @@ public:
 
         // ---- the kept prefix, then the token in it ----
         u64 n = sh.all_c, sum = sh.all_w;
-        const bool cut_k = k > 0 && (u64)k < n;
-        const float p = a.top_p ? a.top_p[r] : 1.f;
-        const double u = (double)a.u[r];
-        // Everything is found among the tokens in front of the first search's end.  Where these fit a list, rank 0 takes them
-        // and does the rest alone.
-        const bool head = take_head(cut_k, cut_k ? (u64)k : p < 1.f ? reach(p, sum) : pass(u, sum));
-        if (head && rank != 0) return;
-        const auto find = [&](bool by_count, u64 target) { return head ? search_head(by_count, target) : search(by_count, target); };
-        if (cut_k) {
-            const Found f = find(true, k);
+        if (k > 0 && (u64)k < n) {
+            const Found f = search(true, k);
             n = k, sum = f.weight;
         }
         if (p < 1.f) {
-            const Found f = find(false, reach(p, sum));
+            const Found f = search(false, reach(p, sum));
             if (f.count < n) n = f.count, sum = f.weight;
         }
         if (mp > 1.f) kept_c = 1, kept_w = (u64)s.unit;   // nobody reaches it: the first token alone
         if (floor_units && kept_c < n) n = kept_c, sum = kept_w;
-        answer(a, r, find(false, pass(u, sum)), n, sum);
+        answer(a, r, search(false, pass(u, sum)), n, sum);
     }
 
 private:
@@ -334,8 +329,6 @@ private:
     const int rank, n_ranks, tid, lane, warp;
     Scale s;
     int turn = 0;
-    int n_head = 0;       // rank 0: tokens of its list,
-    float per_part = 0.f;   // parts a bin of sub_c and sub_w
 
     static __device__ __forceinline__ void bump(uint32_t column, int b, u64 add) {
         const uint32_t at = column + b * (kThreads * 8);
@@ -361,38 +354,229 @@ private:
         if (tid < kBins) sh.bin_w[tid] = w, sh.bin_c[tid] = c;
         if (tid == 0) sh.all_w = tw, sh.all_c = tc;
     }
-    // Rows with a top k: the bins hold counts alone.  Where the tokens up to the k-th's bin fit the list, rank 0 finds everything
-    // among them (min-p too: what it keeps beyond the k-th does not matter) and the row is done.
-    __device__ bool count_bins(const SampleArgs& a, int r, int k) {
-        reduce_bins();
-        sum_bins(exchange());
+    // ---- by estimate ----
+    // Counts of 1024 fine bins (one 32-bit addition in shared memory a token, 11 a clock; weights would be 64-bit ones, of
+    // which there are 1.4) give the place of the k-th token exactly, and, times the weight at a bin's middle, the places where
+    // the running weight reaches what top-p and u ask for to within a fraction of a bin.  One more pass then forms all weights,
+    // sums those in front of each place and takes the tokens of the bins around it; rank 0 finds the tokens among these, and sees
+    // from the exact sums whether they stand there.  Where all tokens up to the last place fit the list, it takes them all.
+    struct Place {
+        int lo, hi;   // fine bins; lo > hi: not asked for
+    };
+    __device__ __forceinline__ int bin_of_count(uint32_t target) const {   // first fine bin at which the count reaches `target`
+        int lo = 0, hi = kFine - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (sh.cum_c[mid] >= target) hi = mid; else lo = mid + 1;
+        }
+        return lo;
+    }
+    __device__ __forceinline__ int bin_of_estimate(float v) const {
+        int lo = 0, hi = kFine - 2;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (sh.cum_e[mid] >= v) hi = mid; else lo = mid + 1;
+        }
+        return lo;
+    }
+    // (a bin's middle is off by half a bin of depth at most, and by a small part of that over many bins)
+    __device__ __forceinline__ Place around(float v) const {
+        const float margin = 0.25f * s.nats + 2e-5f;
+        return Place{max(bin_of_estimate(v * (1.f - margin)) - 1, 0), min(bin_of_estimate(v * (1.f + margin)) + 1, kFine - 2)};
+    }
+    __device__ bool by_estimate(const SampleArgs& a, int r, int k, float p, float mp, double u, u64 floor_units, bool tiny, double least_u) {
+        for (int i = tid; i < kFine; i += kThreads) sh.fine[i] = 0;
         __syncthreads();
-        const u64 live = sh.all_c;
-        if ((u64)k >= live || !take_head(true, (u64)k)) return false;
-        if (rank != 0) return true;
-        Found f = search_head(true, (u64)k);
-        u64 n = k, sum = f.weight;
-        const float p = a.top_p ? a.top_p[r] : 1.f, mp = a.min_p ? a.min_p[r] : 0.f;
+        each8([&](const float(&x)[8], int) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (x[j] > -INFINITY) atomicAdd(&sh.fine[fine_of(s, x[j])], 1u);
+        });
+        cluster.sync();
+        {   // running counts and estimates, two bins a thread
+            static_assert(kFine == 2 * kThreads, "two fine bins a thread");
+            uint32_t c0 = 0, c1 = 0;
+            for (int q = 0; q < n_ranks; ++q) {
+                const uint2 v = reinterpret_cast<const uint2*>(cluster.map_shared_rank(sh.fine, q))[tid];
+                c0 += v.x, c1 += v.y;
+            }
+            const float l2 = -1.4426950f * s.nats;
+            const float e0 = c0 * exp2f(l2 * (2 * tid)), e1 = tid == kThreads - 1 ? 0.f : c1 * exp2f(l2 * (2 * tid + 1));
+            uint32_t pc = c0 + c1;
+            float pe = e0 + e1;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t xc = __shfl_up_sync(0xffffffffu, pc, o);
+                const float xe = __shfl_up_sync(0xffffffffu, pe, o);
+                if (lane >= o) pc += xc, pe += xe;
+            }
+            __syncthreads();
+            if (lane == 31) sh.red_a[warp] = pc, sh.red_b[warp] = __float_as_uint(pe);
+            __syncthreads();
+            for (int q = 0; q < warp; ++q) pc += (uint32_t)sh.red_a[q], pe += __uint_as_float((uint32_t)sh.red_b[q]);
+            sh.cum_c[2 * tid] = pc - c1, sh.cum_c[2 * tid + 1] = pc;
+            sh.cum_e[2 * tid] = pe - e1, sh.cum_e[2 * tid + 1] = pe;
+            __syncthreads();
+        }
+        // ---- the places ----
+        const uint32_t live = sh.cum_c[kFine - 1];
+        const bool cut_k = k > 0 && (uint32_t)k < live;
+        const int bk = cut_k ? bin_of_count(k) : kFine - 1;
+        const bool at_k = bk < kFine - 1;    // (behind it: among the tokens of weight 0, which add nothing)
+        Place at[3] = {{1, 0}, {1, 0}, {1, 0}};   // of the k-th token, of top-p's last, of the one that u picks
+        float v = sh.cum_e[kFine - 2];
+        if (at_k) {
+            at[0] = Place{bk, bk};
+            const uint32_t before = bk ? sh.cum_c[bk - 1] : 0;
+            const float eb = bk ? sh.cum_e[bk - 1] : 0.f;
+            v = eb + (sh.cum_e[bk] - eb) * (float)((uint32_t)k - before) / (float)(sh.cum_c[bk] - before);
+        }
         if (p < 1.f) {
-            f = search_head(false, reach(p, sum));
+            v *= fmaxf(p, 0.f);
+            at[1] = around(v);
+        }
+        if (mp > 0.f) v = fminf(v, sh.cum_e[min((int)fminf(-logf(fminf(mp, 1.f)) / s.nats, 1e6f), kFine - 2)]);
+        at[2] = around(v * (float)u);
+        const int top = at_k ? bk : max(at[1].hi, at[2].hi);
+        const bool head = sh.cum_c[top] <= kList;
+        if (!head) {
+            uint32_t n = 0;
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (at[i].lo <= at[i].hi) n += sh.cum_c[at[i].hi] - (at[i].lo ? sh.cum_c[at[i].lo - 1] : 0);
+            if (n > kList) return false;
+        }
+        // ---- the tokens, and the weights in front of them ----
+        u64* list = reinterpret_cast<u64*>(hist);
+        if (tid == 0) sh.n_list = 0;
+        __syncthreads();
+        const auto take = [&](const float(&x)[8], int i, uint32_t in) {
+            for (; in; in &= in - 1) {
+                const int j = __ffs(in) - 1;
+                list[atomicAdd(&sh.n_list, 1u)] = (u64)order_of(pick(x, j)) << 32 | (uint32_t)(i + j);
+            }
+        };
+        u64 all_w = 0, kept_c = 0, kept_w = 0, front[3] = {0, 0, 0};
+        if (head && at_k) {   // nothing but these matters
+            each8([&](const float(&x)[8], int i) {
+                uint32_t in = 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) in |= (uint32_t)(fine_of(s, x[j]) <= top) << j;
+                take(x, i, in);
+            });
+        } else {
+            const Place a0 = head ? Place{0, top} : at[0], a1 = head ? Place{1, 0} : at[1], a2 = head ? Place{1, 0} : at[2];
+            const auto sum_up = [&](auto with_floor) {
+                each8([&](const float(&x)[8], int i) {
+                    u64 w[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) w[j] = weight_units(s, fmaxf(x[j], s.low));
+                    uint32_t in = 0;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int b = fine_of(s, x[j]);
+                        const u64 units = b < kFine - 1 ? w[j] : 0;
+                        all_w += units;
+                        if (b < a0.lo) front[0] += units;
+                        if (b < a1.lo) front[1] += units;
+                        if (b < a2.lo) front[2] += units;
+                        in |= (uint32_t)((b >= a0.lo && b <= a0.hi) || (b >= a1.lo && b <= a1.hi) || (b >= a2.lo && b <= a2.hi)) << j;
+                        if constexpr (decltype(with_floor)::value) {
+                            const bool keep = x[j] > -INFINITY && (tiny ? ((double)x[j] - s.wide_top) * s.c >= least_u : units >= floor_units);
+                            kept_c += keep, kept_w += keep ? units : 0;
+                        }
+                    }
+                    take(x, i, in);
+                });
+            };
+            if (floor_units) sum_up(std::true_type{});
+            else sum_up(std::false_type{});
+            block_sum(all_w, front[0]);
+            block_sum(front[1], front[2]);
+            block_sum(kept_c, kept_w);
+        }
+        publish(64, all_w), publish(65, front[0]), publish(66, front[1]), publish(67, front[2]), publish(68, kept_c), publish(69, kept_w);
+        const u64(*in)[72] = exchange();
+        if (rank == 0) {
+            all_w = front[0] = front[1] = front[2] = kept_c = kept_w = 0;
+            int n_list = (int)sh.n_list;
+            for (int q = 0; q < n_ranks; ++q) {
+                all_w += in[q][64], front[0] += in[q][65], front[1] += in[q][66], front[2] += in[q][67], kept_c += in[q][68], kept_w += in[q][69];
+                if (q == 0) continue;
+                const int more = (int)*cluster.map_shared_rank(&sh.n_list, q);
+                const u64* from = cluster.map_shared_rank(list, q);
+                for (int i = tid; i < more; i += kThreads) list[n_list + i] = from[i];
+                n_list += more;
+            }
+            __syncthreads();
+            const bool ok = settle(a, r, k, p, mp, u, floor_units, tiny, least_u, at, head, live, at_k, n_list, all_w, front, kept_c, kept_w);
+            if (tid < n_ranks) *cluster.map_shared_rank(&sh.done, tid) = ok;
+        }
+        cluster.sync();
+        return sh.done;
+    }
+    // Rank 0: the searches, over the list.  False where an estimate was too far off.
+    __device__ bool settle(const SampleArgs& a, int r, int k, float p, float mp, double u, u64 floor_units, bool tiny, double least_u,
+                           const Place (&at)[3], bool head, uint32_t live, bool at_k, int n_list, u64 all_w, const u64 (&front)[3],
+                           u64 kept_c, u64 kept_w) {
+        u64 n = k > 0 && (uint32_t)k < live ? k : live, sum = all_w;
+        Found f;
+        const float per_unit = (float)(1.0 / s.unit);
+        if (at_k) {
+            if (!find(true, k, at[0], head, front[0], n_list, f)) return false;
+            sum = f.weight;
+        }
+        if (p < 1.f) {
+            const u64 target = reach(p, sum);
+            if (!find(false, target, head ? around((float)target * per_unit) : at[1], head, front[1], n_list, f)) return false;
             if (f.count < n) n = f.count, sum = f.weight;
         }
         if (mp > 1.f) {
-            n = 1, sum = (u64)s.unit;
-        } else if (mp > 0.f) {
-            const u64 least = (u64)fmin(ceil((double)mp * s.unit), s.unit);
-            const double least_u = 64.0 * log2((double)mp);
+            kept_c = 1, kept_w = (u64)s.unit;   // nobody reaches it: the first token alone
+        } else if (floor_units && head && at_k) {   // (what min-p keeps beyond the k-th does not matter)
             const u64* list = reinterpret_cast<const u64*>(hist);
-            u64 c = 0, w = 0;
-            for (int i = tid; i < n_head; i += kThreads) {
+            kept_c = kept_w = 0;
+            for (int i = tid; i < n_list; i += kThreads) {
                 const float x = value_of((uint32_t)(list[i] >> 32));
                 const u64 units = weight_units(s, x);
-                if (least == 1 ? ((double)x - s.wide_top) * s.c >= least_u : units >= least) c += 1, w += units;
+                if (tiny ? ((double)x - s.wide_top) * s.c >= least_u : units >= floor_units) kept_c += 1, kept_w += units;
             }
-            block_sum(c, w);
-            if (c < n) n = c, sum = w;
+            block_sum(kept_c, kept_w);
         }
-        answer(a, r, search_head(false, pass((double)a.u[r], sum)), n, sum);
+        if (floor_units && kept_c < n) n = kept_c, sum = kept_w;
+        const u64 target = pass(u, sum);
+        if (!find(false, target, head ? around((float)target * per_unit) : at[2], head, front[2], n_list, f)) return false;
+        answer(a, r, f, n, sum);
+        return true;
+    }
+    // search() among the list's tokens of the fine bins of `place`; in front of them stand `front` units of weight, or (head)
+    // the list's own tokens of lower bins
+    __device__ bool find(bool by_count, u64 target, const Place& place, bool head, u64 front, int n_list, Found& f) {
+        const u64* list = reinterpret_cast<const u64*>(hist);
+        u64* found = reinterpret_cast<u64*>(hist) + kList;
+        __syncthreads();   // the last search's list and counter are done with
+        if (tid == 0) sh.n_next = 0;
+        __syncthreads();
+        u64 before = 0, here = 0;
+        for (int i = tid; i < n_list; i += kThreads) {
+            const u64 o = list[i];
+            const float x = value_of((uint32_t)(o >> 32));
+            const int b = fine_of(s, x);
+            if (b > place.hi || (b < place.lo && !head)) continue;
+            const u64 units = b < kFine - 1 ? weight_units(s, x) : 0;
+            if (b < place.lo) {
+                before += units;
+            } else {
+                here += units;
+                found[atomicAdd(&sh.n_next, 1u)] = o;
+            }
+        }
+        block_sum(before, here);
+        if (!head) before = front;
+        const u64 count = place.lo ? sh.cum_c[place.lo - 1] : 0;
+        const int n = (int)sh.n_next;
+        if (n == 0 || (by_count ? target <= count || target > count + n : target <= before || target > before + here)) return false;
+        f = select(by_count, target, count, before, found, n);
         return true;
     }
     // f(eight logits, index of the first) for this CTA's segment, out of shared memory where it is kept there (a thread finds its
@@ -545,75 +729,6 @@ private:
         }
         return n;
     }
-    // Tokens up to the bin that the target falls into, to rank 0's list; false (and nothing done) where they are too many.  On
-    // rank 0 then sub_c, sub_w: running counts and weights of 256 parts of these bins' depths.
-    __device__ bool take_head(bool by_count, u64 target) {
-        u64 base_c, base_w;
-        const int last = bin_reaching(by_count, target, base_c, base_w);
-        if (last == kZeroBin || base_c + sh.bin_c[last] > kList) return false;
-        n_head = collect([&](auto put) {
-            each8([&](const float(&x)[8], int i) {
-                uint32_t in = 0;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) in |= (uint32_t)(bin_of(s, x[j]) <= last) << j;
-                for (; in; in &= in - 1) {
-                    const int j = __ffs(in) - 1;
-                    put((u64)order_of(pick(x, j)) << 32 | (uint32_t)(i + j));
-                }
-            });
-        });
-        if (rank != 0) return true;
-        per_part = 256.f / (last + 1);
-        const u64* list = reinterpret_cast<const u64*>(hist);
-        if (tid < 256) sh.sub_w[tid] = 0, sh.sub_c[tid] = 0;
-        __syncthreads();
-        for (int i = tid; i < n_head; i += kThreads) {
-            const float x = value_of((uint32_t)(list[i] >> 32));
-            const int part = part_of(s, x, -0.5f, per_part, 256);
-            atomicAdd(&sh.sub_c[part], 1u);
-            atomicAdd(&sh.sub_w[part], weight_units(s, x));
-        }
-        __syncthreads();
-        if (warp == 0) {
-            u64 w[8], tw = 0;
-            uint32_t c[8], tc = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = tw += sh.sub_w[lane * 8 + e], c[e] = tc += sh.sub_c[lane * 8 + e];
-            u64 pw = tw;
-            uint32_t pc = tc;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const u64 xw = __shfl_up_sync(0xffffffffu, pw, o);
-                const uint32_t xc = __shfl_up_sync(0xffffffffu, pc, o);
-                if (lane >= o) pw += xw, pc += xc;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sh.sub_w[lane * 8 + e] = w[e] + pw - tw, sh.sub_c[lane * 8 + e] = c[e] + pc - tc;
-        }
-        __syncthreads();
-        return true;
-    }
-    // search() over the head, by rank 0 alone
-    __device__ Found search_head(bool by_count, u64 target) {
-        const uint32_t below = __ballot_sync(0xffffffffu, (by_count ? (u64)sh.sub_c[lane * 8 + 7] : sh.sub_w[lane * 8 + 7]) < target);
-        int part = __popc(below) * 8;   // (running sums ascend)
-        while (part < 255 && (by_count ? (u64)sh.sub_c[part] : sh.sub_w[part]) < target) ++part;
-        part = min(part, 255);
-        const u64 base_c = part ? sh.sub_c[part - 1] : 0, base_w = part ? sh.sub_w[part - 1] : 0;
-        const u64* list = reinterpret_cast<const u64*>(hist);
-        u64* found = reinterpret_cast<u64*>(hist) + kList;
-        __syncthreads();   // the last search's list and counter are done with
-        if (tid == 0) sh.n_next = 0;
-        __syncthreads();
-        for (int i = tid; i < n_head; i += kThreads) {
-            const u64 o = list[i];
-            if (part_of(s, value_of((uint32_t)(o >> 32)), -0.5f, per_part, 256) == part) found[atomicAdd(&sh.n_next, 1u)] = o;
-        }
-        __syncthreads();
-        const int n = (int)sh.n_next;
-        return select(by_count, target, base_c, base_w, found, n);
-    }
-
     // The first token, in order, at which the running count (or weight) reaches `target` (1 <= target <= the total).
     __device__ Found search(bool by_count, u64 target) {
         u64 base_c, base_w;
