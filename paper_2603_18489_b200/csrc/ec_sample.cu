@@ -363,22 +363,14 @@ private:
     struct Place {
         int lo, hi;   // fine bins; lo > hi: not asked for
     };
-    __device__ __forceinline__ int bin_of_count(uint32_t target) const {   // first fine bin at which the count reaches `target`
-        int lo = 0, hi = kFine - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (sh.cum_c[mid] >= target) hi = mid; else lo = mid + 1;
-        }
-        return lo;
+    // First fine bin at which the running value, no longer below `target`, is; whole warps, two loads
+    template <typename V>
+    __device__ __forceinline__ int bin_reaching(const V* cum, V target) const {
+        const int block = min(__popc(__ballot_sync(0xffffffffu, cum[lane * 32 + 31] < target)), 31);
+        return block * 32 + min(__popc(__ballot_sync(0xffffffffu, cum[block * 32 + lane] < target)), 31);
     }
-    __device__ __forceinline__ int bin_of_estimate(float v) const {
-        int lo = 0, hi = kFine - 2;
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (sh.cum_e[mid] >= v) hi = mid; else lo = mid + 1;
-        }
-        return lo;
-    }
+    __device__ __forceinline__ int bin_of_count(uint32_t target) const { return bin_reaching<uint32_t>(sh.cum_c, target); }
+    __device__ __forceinline__ int bin_of_estimate(float v) const { return min(bin_reaching<float>(sh.cum_e, v), kFine - 2); }
     // (a bin's middle is off by half a bin of depth at most, and by a small part of that over many bins)
     __device__ __forceinline__ Place around(float v) const {
         const float margin = 0.25f * s.nats + 2e-5f;
@@ -439,6 +431,10 @@ private:
         at[2] = around(v * (float)u);
         const int top = at_k ? bk : max(at[1].hi, at[2].hi);
         const bool head = sh.cum_c[top] <= kList;
+        // (each begins no later than the next, as it should: the sums in front of them are sums of classes)
+        const bool at_p = p < 1.f;
+        if (at_k && at_p) at[1].lo = min(at[1].lo, bk);
+        at[2].lo = min(at[2].lo, at_p ? at[1].lo : at_k ? bk : at[2].lo);
         if (!head) {
             uint32_t n = 0;
 #pragma unroll
@@ -465,7 +461,13 @@ private:
                 take(x, i, in);
             });
         } else {
-            const Place a0 = head ? Place{0, top} : at[0], a1 = head ? Place{1, 0} : at[1], a2 = head ? Place{1, 0} : at[2];
+            // Classes of tokens: in front of u's place, from there to top-p's, from there to the k-th's, behind; a thread sums the
+            // weights of each in a column of its own.  A token is taken up to the end of the last place that began.
+            const int lo0 = head ? 0 : at[2].lo, lo1 = head || !at_p ? lo0 : at[1].lo, lo2 = head || !at_k ? lo1 : bk;
+            const int hi0 = head ? top : at[2].hi, hi1 = head || !at_p ? hi0 : max(hi0, at[1].hi), hi2 = head || !at_k ? hi1 : max(hi1, bk);
+            const uint32_t column = tc::s2u(hist) + kList * 8 + tid * 8;   // (behind the list)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) sts64(column + c * (kThreads * 8), 0);
             const auto sum_up = [&](auto with_floor) {
                 each8([&](const float(&x)[8], int i) {
                     u64 w[8];
@@ -476,11 +478,9 @@ private:
                     for (int j = 0; j < 8; ++j) {
                         const int b = fine_of(s, x[j]);
                         const u64 units = b < kFine - 1 ? w[j] : 0;
-                        all_w += units;
-                        if (b < a0.lo) front[0] += units;
-                        if (b < a1.lo) front[1] += units;
-                        if (b < a2.lo) front[2] += units;
-                        in |= (uint32_t)((b >= a0.lo && b <= a0.hi) || (b >= a1.lo && b <= a1.hi) || (b >= a2.lo && b <= a2.hi)) << j;
+                        const int c = (b >= lo0) + (b >= lo1) + (b >= lo2);
+                        bump(column, c, units);
+                        in |= (uint32_t)(b >= lo0 && b <= (b >= lo2 ? hi2 : b >= lo1 ? hi1 : hi0)) << j;
                         if constexpr (decltype(with_floor)::value) {
                             const bool keep = x[j] > -INFINITY && (tiny ? ((double)x[j] - s.wide_top) * s.c >= least_u : units >= floor_units);
                             kept_c += keep, kept_w += keep ? units : 0;
@@ -491,6 +491,10 @@ private:
             };
             if (floor_units) sum_up(std::true_type{});
             else sum_up(std::false_type{});
+            front[2] = lds64(column);
+            front[1] = front[2] + lds64(column + kThreads * 8);
+            front[0] = front[1] + lds64(column + 2 * kThreads * 8);
+            all_w = front[0] + lds64(column + 3 * kThreads * 8);
             block_sum(all_w, front[0]);
             block_sum(front[1], front[2]);
             block_sum(kept_c, kept_w);
@@ -558,17 +562,22 @@ private:
         if (tid == 0) sh.n_next = 0;
         __syncthreads();
         u64 before = 0, here = 0;
-        for (int i = tid; i < n_list; i += kThreads) {
-            const u64 o = list[i];
-            const float x = value_of((uint32_t)(o >> 32));
-            const int b = fine_of(s, x);
-            if (b > place.hi || (b < place.lo && !head)) continue;
-            const u64 units = b < kFine - 1 ? weight_units(s, x) : 0;
+        constexpr int kMine = kList / kThreads;
+        u64 o[kMine], w[kMine];
+#pragma unroll
+        for (int e = 0; e < kMine; ++e) o[e] = list[e * kThreads + tid];   // (what stands behind the list is not used)
+#pragma unroll
+        for (int e = 0; e < kMine; ++e) w[e] = weight_units(s, fmaxf(value_of((uint32_t)(o[e] >> 32)), s.low));
+#pragma unroll
+        for (int e = 0; e < kMine; ++e) {
+            const int b = fine_of(s, value_of((uint32_t)(o[e] >> 32)));
+            if (e * kThreads + tid >= n_list || b > place.hi || (b < place.lo && !head)) continue;
+            const u64 units = b < kFine - 1 ? w[e] : 0;
             if (b < place.lo) {
                 before += units;
             } else {
                 here += units;
-                found[atomicAdd(&sh.n_next, 1u)] = o;
+                found[atomicAdd(&sh.n_next, 1u)] = o[e];
             }
         }
         block_sum(before, here);
