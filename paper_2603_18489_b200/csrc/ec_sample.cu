@@ -17,7 +17,7 @@
 
 #include <cooperative_groups.h>
 
-#include <cstdlib>
+#include <cmath>
 #include <type_traits>
 
 namespace ec {
@@ -25,16 +25,13 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-#ifndef EC_ST
-#define EC_ST 512
-#endif
-constexpr int kThreads = EC_ST, kWarps = kThreads / 32;
+constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 16, kZeroBin = kBins - 1;   // the last: weights that round to 0
 constexpr int kBinBits = 4;
 static_assert(1 << kBinBits == kBins, "bins");
 constexpr int kWeightBits = 53;            // of a thread's column of a bin; the rest counts
 constexpr int kMaxCluster = 8;
-constexpr int kSegment = kThreads * 1016;  // elements of a CTA: 1016 weights of 2^43 units fit a thread's column
+constexpr int kSegment = kThreads * 1016;  // tokens of a CTA: 1016 weights of 2^43 units fit a thread's column
 constexpr int kList = kThreads * kBins / 2;   // candidates that a search takes out of the row: two lists of them over the bins
 constexpr int kFew = 128;                  // candidates that are ranked against one another
 constexpr uint32_t HIST_BYTES = kBins * kThreads * 8;
@@ -371,10 +368,14 @@ private:
     }
     __device__ __forceinline__ int bin_of_count(uint32_t target) const { return bin_reaching<uint32_t>(sh.cum_c, target); }
     __device__ __forceinline__ int bin_of_estimate(float v) const { return min(bin_reaching<float>(sh.cum_e, v), kFine - 2); }
-    // (a bin's middle is off by half a bin of depth at most, and by a small part of that over many bins)
-    __device__ __forceinline__ Place around(float v) const {
-        const float margin = 0.25f * s.nats + 2e-5f;
-        return Place{max(bin_of_estimate(v * (1.f - margin)) - 1, 0), min(bin_of_estimate(v * (1.f + margin)) + 1, kFine - 2)};
+    // Around the place where the running weight is `v`.  A bin's estimate is off by a factor of e^(nats / 2) at most, and so is
+    // every running one: `sure`.  With many tokens the errors cancel: a quarter of it, and a bin to either side, nearly always
+    // hold the place; where equal logits fill the bins beside it, a tenth and no further bin.
+    enum Width { sure, usual, narrow };
+    __device__ __forceinline__ Place around(float v, Width width) const {
+        const float margin = (width == sure ? 0.55f : width == usual ? 0.25f : 0.1f) * s.nats + 2e-5f;
+        const int more = width == narrow ? 0 : 1;
+        return Place{max(bin_of_estimate(v * (1.f - margin)) - more, 0), min(bin_of_estimate(v * (1.f + margin)) + more, kFine - 2)};
     }
     __device__ bool by_estimate(const SampleArgs& a, int r, int k, float p, float mp, double u, u64 floor_units, bool tiny, double least_u) {
         for (int i = tid; i < kFine; i += kThreads) sh.fine[i] = 0;
@@ -415,33 +416,34 @@ private:
         const bool cut_k = k > 0 && (uint32_t)k < live;
         const int bk = cut_k ? bin_of_count(k) : kFine - 1;
         const bool at_k = bk < kFine - 1;    // (behind it: among the tokens of weight 0, which add nothing)
-        Place at[3] = {{1, 0}, {1, 0}, {1, 0}};   // of the k-th token, of top-p's last, of the one that u picks
-        float v = sh.cum_e[kFine - 2];
+        const bool at_p = p < 1.f;
+        float v = sh.cum_e[kFine - 2], vp = 0.f;
         if (at_k) {
-            at[0] = Place{bk, bk};
             const uint32_t before = bk ? sh.cum_c[bk - 1] : 0;
             const float eb = bk ? sh.cum_e[bk - 1] : 0.f;
             v = eb + (sh.cum_e[bk] - eb) * (float)((uint32_t)k - before) / (float)(sh.cum_c[bk] - before);
         }
-        if (p < 1.f) {
-            v *= fmaxf(p, 0.f);
-            at[1] = around(v);
-        }
+        if (at_p) v = vp = v * fmaxf(p, 0.f);
         if (mp > 0.f) v = fminf(v, sh.cum_e[min((int)fminf(-logf(fminf(mp, 1.f)) / s.nats, 1e6f), kFine - 2)]);
-        at[2] = around(v * (float)u);
-        const int top = at_k ? bk : max(at[1].hi, at[2].hi);
-        const bool head = sh.cum_c[top] <= kList;
-        // (each begins no later than the next, as it should: the sums in front of them are sums of classes)
-        const bool at_p = p < 1.f;
-        if (at_k && at_p) at[1].lo = min(at[1].lo, bk);
-        at[2].lo = min(at[2].lo, at_p ? at[1].lo : at_k ? bk : at[2].lo);
-        if (!head) {
+        const float vu = v * (float)u;
+        Place at[3];   // of the k-th token, of top-p's last, of the one that u picks
+        const auto places = [&](Width width) {
+            at[0] = at_k ? Place{bk, bk} : Place{1, 0};
+            at[1] = at_p ? around(vp, width) : Place{1, 0};
+            at[2] = around(vu, width);
+            // (each begins no later than the next, as it should: the sums in front of them are sums of classes)
+            if (at_k && at_p) at[1].lo = min(at[1].lo, bk);
+            at[2].lo = min(at[2].lo, at_p ? at[1].lo : at_k ? bk : at[2].lo);
             uint32_t n = 0;
 #pragma unroll
             for (int i = 0; i < 3; ++i)
                 if (at[i].lo <= at[i].hi) n += sh.cum_c[at[i].hi] - (at[i].lo ? sh.cum_c[at[i].lo - 1] : 0);
-            if (n > kList) return false;
-        }
+            return n <= kList;
+        };
+        places(sure);
+        const int top = at_k ? bk : max(at[1].hi, at[2].hi);
+        const bool head = sh.cum_c[top] <= kList;
+        if (!head && !places(usual) && !places(narrow)) return false;
         // ---- the tokens, and the weights in front of them ----
         u64* list = reinterpret_cast<u64*>(hist);
         if (tid == 0) sh.n_list = 0;
@@ -532,7 +534,7 @@ private:
         }
         if (p < 1.f) {
             const u64 target = reach(p, sum);
-            if (!find(false, target, head ? around((float)target * per_unit) : at[1], head, front[1], n_list, f)) return false;
+            if (!find(false, target, head ? around((float)target * per_unit, sure) : at[1], head, front[1], n_list, f)) return false;
             if (f.count < n) n = f.count, sum = f.weight;
         }
         if (mp > 1.f) {
@@ -549,7 +551,7 @@ private:
         }
         if (floor_units && kept_c < n) n = kept_c, sum = kept_w;
         const u64 target = pass(u, sum);
-        if (!find(false, target, head ? around((float)target * per_unit) : at[2], head, front[2], n_list, f)) return false;
+        if (!find(false, target, head ? around((float)target * per_unit, sure) : at[2], head, front[2], n_list, f)) return false;
         answer(a, r, f, n, sum);
         return true;
     }
@@ -894,7 +896,7 @@ private:
 };
 
 template <typename T, bool kResident>
-__global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a, int segment) {
+__global__ void __launch_bounds__(kThreads, kResident ? 1 : 2) sample_kernel(const SampleArgs a, int segment) {
     extern __shared__ __align__(16) unsigned char hist[];   // the bins (or lists), then the segment
     __shared__ Shared sh;
     cg::cluster_group cluster = cg::this_cluster();
@@ -931,16 +933,34 @@ cudaError_t launch_as(const SampleArgs& a, int c, int segment, cudaStream_t stre
     return cudaLaunchKernelEx(&cfg, sample_kernel<T, kResident>, a, segment);
 }
 
+// CTAs of a row, and whether a segment is kept in shared memory (one CTA an SM) or read again from L2 (two).  A CTA takes
+// 14 us and 0.8 us for each 1000 tokens, two on an SM 22 and 1.5; the CTAs that do not fit at once make whole further rounds
+// while these are few.  us, kept with 2 / 4 / 8 CTAs, read again with 2 / 4 / 8: 32 rows of 126464 in fp32 69 40 53, 69 47 46;
+// 256 rows of 152064 in bf16 (not kept with 2) - 300 460, 281 266 -; 128 of 32000 in bf16 49 74 150, 53 58 109; 64 of 126464 in
+// fp32 90 81 130, 90 76 97; 16 of 152064 in bf16 102 73 62, 102 80 71.
+double rounds_us(double ctas, double at_once, double us) {
+    const double r = ctas / at_once;
+    return us * (r <= 3. ? ceil(r) : r);
+}
 template <typename T>
 cudaError_t launch(const SampleArgs& a, cudaStream_t stream) {
-    // CTAs of a row: enough that a segment stays in shared memory beside the bins, and all SMs at work while rows are few
-    int c = 1;
-    const auto segment = [&](int n) { return ((a.vocab + n - 1) / n + 7) & ~7; };
-    const auto fits = [&](int n) { return (int)HIST_BYTES + (long long)segment(n) * (int)sizeof(T) <= kMaxDynamic; };
-    while (c < kMaxCluster && !fits(c)) c *= 2;
-    if (const char* e = getenv("EC_SC")) c = atoi(e);
-    while (c < kMaxCluster && (long long)a.n_rows * c * 2 <= sm_count() + 4 && a.vocab > c * 4096) c *= 2;
-    return fits(c) ? launch_as<T, true>(a, c, segment(c), stream) : launch_as<T, false>(a, c, segment(c), stream);
+    const auto segment = [&](int c) { return ((a.vocab + c - 1) / c + 7) & ~7; };
+    const double sms = sm_count();
+    int best_c = kMaxCluster;
+    bool kept = false;
+    double best = 1e30;
+    for (int c = 1; c <= kMaxCluster; c *= 2) {
+        const int seg = segment(c);
+        if (seg > kSegment || (c > 1 && seg < 1024)) continue;
+        const double ctas = (double)a.n_rows * c;
+        if ((int)HIST_BYTES + (long long)seg * (int)sizeof(T) <= kMaxDynamic) {
+            const double us = rounds_us(ctas, sms, 14. + 8e-4 * seg);
+            if (us < best) best = us, best_c = c, kept = true;
+        }
+        const double us = ctas <= sms ? 14. + 1.05e-3 * seg : rounds_us(ctas, 2. * sms, 22. + 1.5e-3 * seg);
+        if (us < best) best = us, best_c = c, kept = false;
+    }
+    return kept ? launch_as<T, true>(a, best_c, segment(best_c), stream) : launch_as<T, false>(a, best_c, segment(best_c), stream);
 }
 
 }  // namespace
