@@ -10,13 +10,12 @@
 // angle (2^-25 of half a turn) is put back to first order: 5e-8 of an fp32 result.
 #include "ec_common.cuh"
 #include "ec_tc_ptx.cuh"
-#include <cstdlib>
 
 namespace ec {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxTokens = 32;   // rows a CTA, at most
+constexpr int kMaxTokens = 8;   // rows a CTA, at most
 
 __device__ __forceinline__ void load8(const float* p, float* v) {
     const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
@@ -189,8 +188,7 @@ template <typename T, int HD, bool kPaged>
 cudaError_t launch(const RopeArgs& a, cudaStream_t stream) {
     // Few rows: one a CTA.  Many: the angles' 64-bit arithmetic and the start of a CTA are shared by several.
     int tokens = 1;
-    const int top = getenv("EC_RT") ? atoi(getenv("EC_RT")) : kMaxTokens;
-    while (tokens < top && (long long)a.n_rows > 8ll * sm_count() * tokens) tokens *= 2;
+    while (tokens < kMaxTokens && (long long)a.n_rows > 8ll * sm_count() * tokens) tokens *= 2;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((a.n_rows + tokens - 1) / tokens, 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
