@@ -10,11 +10,12 @@
 //   warps 2-17  softmax, four warpgroups: (row tile) x (64-column half); no running maximum in the first pass, a row's
 //               reference is its largest score among the first eight keys of the part that it sees.  They also bring Q into
 //               shared memory (packed rows are rows of several heads and tokens: plain loads, the swizzle by hand)
-//   warp 18     zeroes the rows of the last V tile that stand behind the sequence's end (an unfinished page may hold anything,
-//               and 0 x NaN is NaN), and looks up the next unit meanwhile
-// A row sees keys below its limit; a tile whose keys are below the lowest limit of a warp's rows needs no mask.
-// Barriers are set up anew for every unit.  A unit that a cut divides leaves its un-normalised rows in the workspace, 16-byte
-// pieces swizzled by row as they stand in shared memory, for the second launch to join.
+// The issuer zeroes the rows of the last V tile that stand behind the sequence's end (an unfinished page may hold anything, and
+// 0 x NaN is NaN).  A row sees keys below its limit; a tile whose keys are below the lowest limit of a warp's rows needs no mask.
+// The roles go from unit to unit by themselves: the producer, which is ahead of the others, writes down what the next unit is
+// (four places, B_SEGFULL and B_SEGFREE), barriers and ring go on, and so the next unit's keys are on their way while this one's
+// rows are still written (@@).  A unit that a cut divides leaves its un-normalised rows in the workspace, columns by fours with
+// the row fastest, as the threads hold them, for the second launch to join.
 #include "ec_paged.cuh"
 #include "ec_paged_combine.cuh"
 #include "ec_tc_ptx.cuh"
@@ -26,9 +27,10 @@ using namespace tc;
 using namespace paged;
 
 constexpr int BM = 128, BN = 128;
-constexpr int kSoftThreads = 512, kThreads = 64 + kSoftThreads + 32;
+constexpr int kSoftThreads = 512, kThreads = 64 + kSoftThreads;
 constexpr uint32_t SUB = 128 * 128;   // [128 rows x 64 bf16], 128-byte swizzle: 16 KB
 constexpr int kSlots = 5;
+constexpr int kSegments = 4;
 struct Segment {   // what the roles know of the unit at hand
     Unit u;
     int j0, j1;    // key tiles of this CTA
@@ -44,15 +46,16 @@ struct Geo {
     static constexpr uint32_t OFF_XCH = OFF_SEG + 256;
     static constexpr uint32_t NEEDED = OFF_XCH + 2 * 2 * BM * 4;
     static constexpr uint32_t BYTES = HD == 128 ? 232448 : NEEDED + 1024;
-    static constexpr uint32_t PART = BM * HD * 4;
-    static_assert(2 * sizeof(Segment) <= 256 && NEEDED + 256 <= BYTES, "shared memory");
-    static_assert((EC_PAGED_MAX_BATCH + 1) * 8 <= kSlots * TILE && 2 * PART <= kSlots * TILE, "what stands over the ring");
+    static_assert(kSegments * sizeof(Segment) <= 256 && NEEDED + 256 <= BYTES, "shared memory");
+    static_assert((EC_PAGED_MAX_BATCH + 1) * 8 <= kSlots * TILE, "what stands over the ring at the start");
 };
 constexpr uint32_t TM_COLS = 512;
 constexpr uint32_t TM_S = 0, TM_O = 256;
 
 enum { B_FULL = 0, B_FREE = kSlots, B_SFULL = B_FREE + 3, B_PFULL = B_SFULL + 2, B_PVDONE = B_PFULL + 4,
-       B_QFULL = B_PVDONE + 2, B_VERDICT = B_QFULL + 2, B_VREADY = B_VERDICT + 1, B_VZERO = B_VREADY + 1, B_COUNT = B_VZERO + 1 };
+       B_QFULL = B_PVDONE + 2, B_VERDICT = B_QFULL + 2, B_SEGFULL = B_VERDICT + 1, B_SEGFREE = B_SEGFULL + kSegments,
+       B_COUNT = B_SEGFREE + kSegments };
+static_assert(B_COUNT * 8 + 24 <= 256, "barriers and flags");
 
 constexpr float kMaxSum = 1.152921504606846976e18f;   // 2^60
 
@@ -66,12 +69,6 @@ struct Params {
     int page_shift, n_pages, max_pages, n_q_heads;
     float scale_log2;
 };
-
-__device__ __forceinline__ void mbar_inval(uint32_t bar) { asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
-__device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t bytes) {
-    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 // packed rows of a unit
@@ -98,11 +95,22 @@ struct Places {
     }
 };
 
+// what the roles need of a unit
+struct Job {
+    int j0, T, kv, rows, n_tiles_q;   // first key tile, key tiles, keys of the sequence, packed rows, row tiles
+    // One row tile: the two halves of the CTA take its even and its odd key tiles, each with a reference and an accumulator of
+    // its own, so that the softmax of one tile runs under the products of the other; the rows are joined at the end.
+    bool split;
+    __device__ __forceinline__ Job(const Plan& p, const Segment& seg)
+        : j0(uniform(seg.j0)), T(uniform(seg.j1) - j0), kv(uniform(seg.u.s.kv)), rows(uniform(rows_of(p, seg.u))),
+          n_tiles_q(rows > BM ? 2 : 1), split(n_tiles_q == 1 && T > 1) {}
+};
+
 template <int HD>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Params p) {
     constexpr uint32_t TILE = Geo<HD>::TILE, OFF_Q = Geo<HD>::OFF_Q, OFF_RING = Geo<HD>::OFF_RING, OFF_BAR = Geo<HD>::OFF_BAR,
-                       OFF_XCH = Geo<HD>::OFF_XCH, PART = Geo<HD>::PART;
+                       OFF_XCH = Geo<HD>::OFF_XCH;
     constexpr int CW = HD / 2, CH = CW / 8, HALVES = HD / 64;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t base = (s2u(smem_raw) + 1023u) & ~1023u;
@@ -110,8 +118,9 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
     const uint32_t bars = base + OFF_BAR;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gbase + OFF_BAR + B_COUNT * 8);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(gbase + OFF_BAR + B_COUNT * 8 + 4);
-    volatile int* again = reinterpret_cast<volatile int*>(gbase + OFF_BAR + B_COUNT * 8 + 8);
-    Segment* segments = reinterpret_cast<Segment*>(gbase + Geo<HD>::OFF_SEG);   // [2]
+    volatile int* again = reinterpret_cast<volatile int*>(gbase + OFF_BAR + B_COUNT * 8 + 8);   // [2], by unit
+    volatile int* go = again + 2;   // [2], by unit
+    Segment* segments = reinterpret_cast<Segment*>(gbase + Geo<HD>::OFF_SEG);   // [kSegments]
     float* xch = reinterpret_cast<float*>(gbase + OFF_XCH);
     int32_t* const dev_status = p.plan.dev_status;
     auto bar = [&](int idx) { return bars + idx * 8; };
@@ -121,15 +130,12 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
     }
     const int tid = threadIdx.x, warp = warp_index(), lane = tid & 31, cta = blockIdx.x;
 
-    auto set_up = [&]() {
-        for (int i = 0; i < B_COUNT; ++i)
-            mbar_init(bar(i), (i >= B_PFULL && i < B_PFULL + 4) || (i >= B_QFULL && i < B_QFULL + 2) ? 256u : 1u);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    };
     if (tid == 0) {
         prefetch_map(&map_k);
         prefetch_map(&map_v);
-        set_up();
+        for (int i = 0; i < B_COUNT; ++i)
+            mbar_init(bar(i), (i >= B_PFULL && i < B_PFULL + 4) || (i >= B_QFULL && i < B_QFULL + 2) ? 256u : i >= B_SEGFREE ? 17u : 1u);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         *abort_flag = 0;
     }
     if (warp == 1) {
@@ -162,6 +168,7 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
             s.j0 = step_at(p.plan, s.u, first);
             s.j1 = step_at(p.plan, s.u, last);
             if (cta == 0) p.cuts[gridDim.x] = cut_of_end(all);
+            mbar_arrive(bar(B_SEGFULL));
         }
     }
     fence_async_smem();   // the ring is the TMA's from here on
@@ -169,21 +176,20 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
     fence_after();
     const uint32_t tmem = *tmem_slot;
 
-    for (int at = 0; segments[at].more; at ^= 1) {
-        const Segment& seg = segments[at];
-        // (values out of shared memory are not warp-uniform to the compiler, and then neither is anything in a loop over them: see
-        // elect_one on what that costs the issuer)
-        const int j0 = uniform(seg.j0), T = uniform(seg.j1) - j0, kv = uniform(seg.u.s.kv), rows = uniform(rows_of(p.plan, seg.u));
-        const int n_tiles_q = rows > BM ? 2 : 1;
-        // One row tile: the two halves of the CTA take its even and its odd key tiles, each with a reference and an accumulator of
-        // its own, so that the softmax of one tile runs under the products of the other; the rows are joined at the end.
-        const bool split = n_tiles_q == 1 && T > 1;
-        const int n_chains = split ? 2 : n_tiles_q;
-        // the tile that the sequence ends inside of, counted from j0; T or more: not here
-        const int j_end = (kv & (BN - 1)) || kv == 0 ? kv / BN - j0 : T;
-
-        if (warp == 0) {
-            // ================================ TMA producer ======================================
+    // (values out of shared memory are not warp-uniform to the compiler, and then neither is anything in a loop over them: see
+    // elect_one on what that costs the issuer; for the same reason each role has its loop over the units and its state to itself)
+    if (warp == 0) {
+        // ================================ TMA producer ======================================
+        // ring slot, the group that frees it and the phase of that barrier; ring entries so far, as far as they matter
+        int slot = 0, group_free = 0, entries = 0;
+        uint32_t turn = 0;
+        for (int it = 0;; ++it) {
+            const Segment& seg = segments[it % kSegments];
+            mbar_wait_warp(bar(B_SEGFULL + it % kSegments), (it / kSegments) & 1, abort_flag, dev_status);
+            if (*abort_flag || !uniform(seg.more)) break;
+            const Job job(p.plan, seg);
+            const int j0 = job.j0, T = job.T, kv = job.kv;
+            const bool split = job.split;
             const bool elected = elect_one();
             const int32_t* table = p.page_table + (long long)seg.u.b * p.max_pages;
             const int ps = 1 << p.page_shift, boxes_page = ps == BN ? 1 : HALVES;
@@ -200,12 +206,27 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
             // Ring entries, from 2T on those of the second pass: K_0 V_0 K_1 V_1 ..., with split K_0 K_1 V_0 K_2 V_1 ... V_T-2 V_T-1.
             // A K tile's pages are looked up one K tile ahead; those of the V tiles to come are kept: one, with split
             // that of the tile before too.
-            int slot = 0, group_free = 0, ahead = page_of(0), kept = -1, kept_next = -1;
-            uint32_t turn = 0;
+            int ahead = page_of(0), kept = -1, kept_next = -1;
             for (int n = 0; n < 4 * T; ++n) {
                 if (n == 2 * T) {
-                    mbar_wait_warp(bar(B_VERDICT), 0, abort_flag, dev_status);
-                    if (!*again) break;
+                    // the next unit, for all
+                    const int nx = (it + 1) % kSegments;
+                    if (it + 1 >= kSegments) mbar_wait_warp(bar(B_SEGFREE + nx), ((it + 1) / kSegments - 1) & 1, abort_flag, dev_status);
+                    if (*abort_flag) break;   // (nothing is written over while somebody may read it)
+                    if (lane == 0) {
+                        Segment s = seg;
+                        s.more = s.u.w0 + s.u.steps + p.plan.start < last;
+                        if (s.more) {
+                            step_unit(p.plan, s.u);
+                            s.j0 = 0;
+                            s.j1 = step_at(p.plan, s.u, last);
+                        }
+                        segments[nx] = s;
+                        mbar_arrive(bar(B_SEGFULL + nx));
+                    }
+                    __syncwarp();
+                    mbar_wait_warp(bar(B_VERDICT), it & 1, abort_flag, dev_status);
+                    if (!again[it & 1]) break;
                     ahead = page_of(0);
                 }
                 const int m = n >= 2 * T ? n - 2 * T : n;
@@ -225,8 +246,9 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                     else kept = page;
                     ahead = page_of(j + 1);
                 }
-                if (n > kSlots && !(n & 1) && ++group_free == 3) group_free = 0, turn ^= 1;
-                if (n >= kSlots) mbar_wait_warp(bar(B_FREE + group_free), turn, abort_flag, dev_status);
+                // (entries of all units count: an even number each)
+                if (entries + n > kSlots && !(n & 1) && ++group_free == 3) group_free = 0, turn ^= 1;
+                if (entries + n >= kSlots) mbar_wait_warp(bar(B_FREE + group_free), turn, abort_flag, dev_status);
                 const int keys = min(max(kv - (j0 + j) * BN, 0), BN), pages = (keys + ps - 1) >> p.page_shift;
                 if (elected) mbar_expect_tx(bar(B_FULL + slot), (uint32_t)(pages << p.page_shift) * (HD * 2));
                 __syncwarp();
@@ -236,10 +258,24 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                 __syncwarp();
                 if (++slot == kSlots) slot = 0;
             }
+            entries = min(entries + (uniform(again[it & 1]) ? 4 : 2) * T, 2 * kSlots);   // (even, and more than the ring holds)
             if (__any_sync(0xffffffffu, bad) && elected && dev_status) atomicExch(dev_status, (int)EC_ERR_PAGE);
             __syncwarp();
-        } else if (warp == 1) {
-            // ================================ MMA issuer ========================================
+        }
+    } else if (warp == 1) {
+        // ================================ MMA issuer ========================================
+        // ring slot and phase of the next tile, the next group to release; by row tile, the phases of P and of Q
+        int slot = 0, group_free = 0;
+        uint32_t phase = 0, p_phase = 0, q_phase = 0;
+        for (int it = 0;; ++it) {
+            const Segment& seg = segments[it % kSegments];
+            mbar_wait_warp(bar(B_SEGFULL + it % kSegments), (it / kSegments) & 1, abort_flag, dev_status);
+            if (*abort_flag || !uniform(seg.more)) break;
+            const Job job(p.plan, seg);
+            const int j0 = job.j0, T = job.T, kv = job.kv, n_tiles_q = job.n_tiles_q;
+            const bool split = job.split;
+            // the tile that the sequence ends inside of, counted from j0; T or more: not here
+            const int j_end = (kv & (BN - 1)) || kv == 0 ? kv / BN - j0 : T;
             const bool elected = elect_one();
             constexpr uint32_t IDESC_S = instr_desc(BN, 0), IDESC_PV = instr_desc(HD, 1);
             const uint64_t desc_q = smem_desc(base + OFF_Q, 16, 1024);
@@ -265,13 +301,15 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                     }
                 }
             };
-            // a V tile that the sequence ends in has landed: the zeroing warp's turn (it could not tell the phases of a ring slot apart)
-            auto zeroed = [&](int pass) {
-                if (elected) mbar_arrive(bar(B_VREADY));
-                mbar_wait_warp(bar(B_VZERO), pass, abort_flag, dev_status);
+            // a V tile that the sequence ends in has landed: rows behind the end become zero
+            auto zeroed = [&](int slot_v) {
+                unsigned char* v = gbase + OFF_RING + slot_v * TILE;
+                for (int i = (kv - (j0 + j_end) * BN) * 8 + lane; i < BN * 8; i += 32)
+#pragma unroll
+                    for (int hf = 0; hf < HALVES; ++hf) *reinterpret_cast<uint4*>(v + hf * SUB + i * 16) = make_uint4(0, 0, 0, 0);
+                fence_async_smem();
+                __syncwarp();
             };
-            int slot = 0, group_free = 0;
-            uint32_t phase = 0, p_phase = 0;
             auto full = [&](int ahead) {
                 const bool wrapped = slot + ahead >= kSlots;
                 return mbar_test(bar(B_FULL + slot + ahead - (wrapped ? kSlots : 0)), phase ^ (wrapped ? 1u : 0u));
@@ -289,13 +327,13 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
             constexpr int kPeek = HD / 16 - 2;
             for (int pass = 0; pass < 2; ++pass) {
                 if (pass == 1) {
-                    mbar_wait_warp(bar(B_VERDICT), 0, abort_flag, dev_status);
-                    if (!*again) break;
+                    mbar_wait_warp(bar(B_VERDICT), it & 1, abort_flag, dev_status);
+                    if (!again[it & 1]) break;
                 }
                 if (split) {
                     for (int t = 0; t < 2; ++t) {   // both chains have Q_0
                         const uint64_t desc_k = smem_desc(base + OFF_RING + take(false) * TILE, 16, 1024);
-                        mbar_wait_warp(bar(B_QFULL), 0, abort_flag, dev_status);
+                        mbar_wait_warp(bar(B_QFULL), q_phase & 1, abort_flag, dev_status);
                         fence_after();
                         scores(t, desc_q, desc_k, 0, HD / 16);
                         if (elected) commit(bar(B_SFULL + t));
@@ -303,8 +341,9 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                     }
                     for (int j = 0; j < T; ++j) {
                         const int t = j & 1;
-                        const uint64_t desc_v = smem_desc(base + OFF_RING + take(false) * TILE, SUB, 1024);
-                        if (j == j_end) zeroed(pass);
+                        const int slot_v = take(false);
+                        const uint64_t desc_v = smem_desc(base + OFF_RING + slot_v * TILE, SUB, 1024);
+                        if (j == j_end) zeroed(slot_v);
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             mbar_wait_warp(bar(B_PFULL + h * 2 + t), (p_phase >> t) & 1, abort_flag, dev_status);
@@ -325,7 +364,7 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                 {
                     const uint64_t desc_k = smem_desc(base + OFF_RING + take(false) * TILE, 16, 1024);
                     for (int t = 0; t < n_tiles_q; ++t) {
-                        mbar_wait_warp(bar(B_QFULL + t), 0, abort_flag, dev_status);
+                        mbar_wait_warp(bar(B_QFULL + t), (q_phase >> t) & 1, abort_flag, dev_status);
                         fence_after();
                         products_s(t, desc_k, 0, HD / 16);
                         if (elected) commit(bar(B_SFULL + t));
@@ -333,23 +372,25 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                     release();
                 }
                 bool kv_ready = false, p_ready = false;
-                for (int j = 0; j < T; ++j, p_phase ^= 1) {
+                for (int j = 0; j < T; ++j) {
                     const bool more = j + 1 < T, more2 = j + 2 < T;
-                    const uint64_t desc_v = smem_desc(base + OFF_RING + take(kv_ready) * TILE, SUB, 1024);
+                    const int slot_v = take(kv_ready);
+                    const uint64_t desc_v = smem_desc(base + OFF_RING + slot_v * TILE, SUB, 1024);
                     const uint64_t desc_k = smem_desc(base + OFF_RING + (more ? take(kv_ready) : 0) * TILE, 16, 1024);
-                    if (j == j_end) zeroed(pass);
+                    if (j == j_end) zeroed(slot_v);
                     for (int t = 0; t < n_tiles_q; ++t) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            if (h == 1 || !p_ready) mbar_wait_warp(bar(B_PFULL + h * 2 + t), p_phase, abort_flag, dev_status);
+                            if (h == 1 || !p_ready) mbar_wait_warp(bar(B_PFULL + h * 2 + t), (p_phase >> t) & 1, abort_flag, dev_status);
                             fence_after();
                             outputs(t, desc_v, h, j > 0);
                         }
+                        p_phase ^= 1u << t;
                         p_ready = false;
                         if (more) {
                             products_s(t, desc_k, 0, kPeek);
-                            const bool next_tile = t + 1 == n_tiles_q;
-                            const bool p_seen = mbar_test(bar(B_PFULL + (next_tile ? 0 : t + 1)), p_phase ^ (next_tile ? 1u : 0u));
+                            const int next = t + 1 == n_tiles_q ? 0 : t + 1;
+                            const bool p_seen = mbar_test(bar(B_PFULL + next), (p_phase >> next) & 1);
                             if (t == 0) kv_ready = __all_sync(0xffffffffu, full(0) && (!more2 || full(1)));
                             p_ready = __all_sync(0xffffffffu, p_seen);
                             products_s(t, desc_k, kPeek, HD / 16);
@@ -360,9 +401,25 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                     if (more) release();
                 }
             }
+            q_phase ^= n_tiles_q == 2 ? 3u : 1u;
             __syncwarp();
-        } else if (warp < 2 + kSoftThreads / 32) {
-            // ================================ softmax (warps 2..17) ================================
+            if (lane == 0) mbar_arrive(bar(B_SEGFREE + it % kSegments));
+        }
+    } else {
+        // ================================ softmax (warps 2..17) ================================
+        uint32_t s_phase = 0, pv_phase = 0;   // of S, and by row tile of the finished products
+        for (int it = 0;; ++it) {
+            const Segment& seg = segments[it % kSegments];
+            // one thread decides for these warps: named barriers know no time-out, so none of them may leave alone
+            if (tid == 64) {
+                mbar_wait(bar(B_SEGFULL + it % kSegments), (it / kSegments) & 1, abort_flag, dev_status);
+                go[it & 1] = !*abort_flag && seg.more;
+            }
+            named_barrier(12, kSoftThreads);
+            if (!uniform(go[it & 1])) break;
+            const Job job(p.plan, seg);
+            const int j0 = job.j0, T = job.T, kv = job.kv, rows = job.rows, n_chains = job.split ? 2 : job.n_tiles_q;
+            const bool split = job.split;
             const int ws = warp - 2;
             const int t = ws >> 3, h = (ws >> 2) & 1;
             const int quarter = warp & 3;
@@ -411,7 +468,8 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                     f32x2 mneg2 = pk(0.f, 0.f), sum2[2] = {pk(0.f, 0.f), pk(0.f, 0.f)};
                     int key0 = (j0 + jt) * BN;   // of the tile
                     for (int i = 0; i < nt; ++i, key0 += js * BN) {
-                        mbar_wait(bar(B_SFULL + t), i & 1, abort_flag, dev_status);
+                        mbar_wait(bar(B_SFULL + t), s_phase, abort_flag, dev_status);
+                        s_phase ^= 1;
                         fence_after();
                         if (i == 0) {
                             uint32_t r8[8];
@@ -474,9 +532,9 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                     upk(sum2[1], b0, b1);
                     l_run = (a0 + a1) + (b0 + b1);
                 }
-                const bool redo = named_barrier_or(9, n_chains * 256, !(l_run <= kMaxSum));
+                const bool redo = named_barrier_or(n_chains == 2 ? 9 : 11, n_chains * 256, !(l_run <= kMaxSum));
                 if (ws == 0 && lane == 0) {
-                    *again = redo ? 1 : 0;
+                    again[it & 1] = redo ? 1 : 0;
                     mbar_arrive(bar(B_VERDICT));
                 }
                 // ---- second pass, only if a score left the first one's range: running maxima ----
@@ -484,9 +542,12 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                     m_used = -INFINITY;
                     l_run = 0.f;
                 }
-                const uint32_t last_phase = redo ? nt & 1 : 0;
+                // B_PVDONE: one phase at the end of the first pass, one per key tile of the second
+                const uint32_t pv0 = (pv_phase >> t) & 1, last_phase = pv0 ^ (redo ? nt & 1 : 0);
+                pv_phase ^= (redo ? (nt + 1) & 1 : 1) << t;
                 for (int i = 0; redo && i < nt; ++i) {
-                    mbar_wait(bar(B_SFULL + t), (nt + i) & 1, abort_flag, dev_status);
+                    mbar_wait(bar(B_SFULL + t), s_phase, abort_flag, dev_status);
+                    s_phase ^= 1;
                     fence_after();
                     uint32_t sr[BN / 2];
                     ld32(tm_s + h * 64, sr);
@@ -533,7 +594,7 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                         l_run = fmaf(l_run, factor, (a0 + a1) + (b0 + b1));
                     }
                     if (need_rescale) {
-                        mbar_wait(bar(B_PVDONE + t), i & 1, abort_flag, dev_status);
+                        mbar_wait(bar(B_PVDONE + t), pv0 ^ (i & 1), abort_flag, dev_status);
                         fence_after();
 #pragma unroll
                         for (int c = 0; c < CW / 32; ++c) {
@@ -619,73 +680,27 @@ attend_paged_tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                         }
                     }
                 } else if (writes) {
-                    // a part: un-normalised rows (relative to m_used), m and l; over the ring, so all products have to be through
-                    if (!split)
-                        for (int tt = 0; tt < n_tiles_q; ++tt) mbar_wait(bar(B_PVDONE + tt), last_phase, abort_flag, dev_status);
+                    // a part: un-normalised rows (relative to m_used), m and l
                     float* part = p.partial + ((long long)cta * 2 + (j0 == 0 ? 1 : 0)) * (2 * BM * (HD + 2));
-                    const bool any = t * BM + quarter * 32 < rows;   // of this warp's rows
-                    if (any) {
-                        unsigned char* prow = gbase + OFF_RING + t * PART + row * (HD * 4);
+                    if (t * BM + quarter * 32 < rows && !*abort_flag) {   // some of this warp's rows
+                        float4* at = reinterpret_cast<float4*>(part) + ((t * (HD / 4) + h * (HD / 8)) * BM + row);
 #pragma unroll 1
                         for (int c = 0; c < CW / 32; ++c) {
                             uint32_t o[32];
                             columns(c, o);
 #pragma unroll
                             for (int v4 = 0; v4 < 8; ++v4)
-                                *reinterpret_cast<uint4*>(prow + (((h * (HD / 8) + c * 8 + v4) ^ (row & (HD / 4 - 1))) << 4)) =
-                                    make_uint4(o[v4 * 4], o[v4 * 4 + 1], o[v4 * 4 + 2], o[v4 * 4 + 3]);
+                                at[(c * 8 + v4) * BM] = make_float4(__uint_as_float(o[v4 * 4]), __uint_as_float(o[v4 * 4 + 1]),
+                                                                    __uint_as_float(o[v4 * 4 + 2]), __uint_as_float(o[v4 * 4 + 3]));
                         }
                         if (h == 0)   // (no weight on the reference of a row that saw nothing)
                             *reinterpret_cast<float2*>(part + 2 * BM * HD + (t * BM + row) * 2) = make_float2(l_row > 0.f ? m_used : -INFINITY, l_row);
-                        fence_async_smem();
-                        named_barrier(pair_bar, 64);
-                        if (h == 0 && lane == 0 && !*abort_flag) {
-                            bulk_store(part + (t * BM + quarter * 32) * HD, base + OFF_RING + t * PART + quarter * 32 * (HD * 4), 32 * HD * 4);
-                            bulk_commit();
-                            bulk_wait();
-                        }
                     }
                 }
             }
             fence_before();
-        } else {
-            // ====================== the last V tile's rows behind the end; the next unit ============================
-            for (int pass = 0; pass < 2 && j_end < T; ++pass) {
-                if (pass == 1) {
-                    mbar_wait_warp(bar(B_VERDICT), 0, abort_flag, dev_status);
-                    if (!*again) break;
-                }
-                const int n = 2 * j_end + (split && j_end < T - 1 ? 2 : 1) + pass * 2 * T;   // its ring entry
-                mbar_wait_warp(bar(B_VREADY), pass, abort_flag, dev_status);
-                unsigned char* v = gbase + OFF_RING + n % kSlots * TILE;
-                const int r0 = kv - (j0 + j_end) * BN;   // first row behind the end
-                for (int i = r0 * 8 + lane; i < BN * 8; i += 32)
-#pragma unroll
-                    for (int hf = 0; hf < HALVES; ++hf) *reinterpret_cast<uint4*>(v + hf * SUB + i * 16) = make_uint4(0, 0, 0, 0);
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(B_VZERO));
-            }
-            if (lane == 0) {
-                Segment s = seg;
-                s.more = s.u.w0 + s.u.steps + p.plan.start < last;
-                if (s.more) {
-                    step_unit(p.plan, s.u);
-                    s.j0 = 0;
-                    s.j1 = step_at(p.plan, s.u, last);
-                }
-                segments[at ^ 1] = s;
-            }
-        }
-        __syncthreads();
-        if (*abort_flag) break;   // (the same for all: read behind the barrier, written before it)
-        if (segments[at ^ 1].more) {
-            if (tid == 0) {
-                for (int i = 0; i < B_COUNT; ++i) mbar_inval(bar(i));
-                set_up();
-            }
-            __syncthreads();
-            fence_after();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(B_SEGFREE + it % kSegments));
         }
     }
 

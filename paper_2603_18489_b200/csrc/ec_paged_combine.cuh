@@ -19,8 +19,8 @@ __device__ __forceinline__ void store4(__nv_bfloat16* dst, const float* v, float
 constexpr int kCombineThreads = 512;
 constexpr int kMaxWeights = 2048;   // 2 x 256, and 256 + 2 x the parts (at most one a CTA)
 
-// partial: [worker][2 slots] of { rows [tm][HD], then (maximum, sum) [tm] }; kSwizzled: 16-byte piece c of row r at c ^ r
-template <typename T, int HD, bool kSwizzled>
+// partial: [worker][2 slots] of { rows [tm][HD], then (maximum, sum) [tm] }; kColumns: the rows of every 128 as [HD / 4][128][4]
+template <typename T, int HD, bool kColumns>
 __global__ void __launch_bounds__(kCombineThreads) attend_paged_combine_kernel(const Plan p, const Cut* cuts,
                                                                                const float* partial, T* out, int n_q_heads,
                                                                                int ctas) {
@@ -71,24 +71,54 @@ __global__ void __launch_bounds__(kCombineThreads) attend_paged_combine_kernel(c
         for (int k = 0; k < parts; ++k) weight[i * parts + k] *= inv;
     }
     __syncthreads();
+    if constexpr (kColumns) {
+        // Eight rows and 64 columns a warp, a lane sixteen columns of a row: its four loads of a part are 128 contiguous bytes of
+        // eight lanes, its two stores a sector.  (A row a warp, as below: 32 lines a load, 256 rows over 4096 keys 59 us, @@.)
+        for (int item = warp; item < (mine + 7) / 8 * (HD / 64); item += kCombineThreads / 32) {
+            const int i = item / (HD / 64) * 8 + (lane & 7), r = row0 + min(i, mine - 1), piece = item % (HD / 64) * 16 + (lane >> 3) * 4;
+            const long long off = (((r >> 7) * (HD / 4) + piece) * 128 + (r & 127)) * 4;
+            float acc[16] = {};
+#pragma unroll 2
+            for (int k = 0; k < parts; ++k) {
+                const float* src = part_at(k) + off;
+                float4 x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const float4*>(src + e * 512);
+                const float f = weight[min(i, mine - 1) * parts + k];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    acc[4 * e] = fmaf(f, x[e].x, acc[4 * e]), acc[4 * e + 1] = fmaf(f, x[e].y, acc[4 * e + 1]);
+                    acc[4 * e + 2] = fmaf(f, x[e].z, acc[4 * e + 2]), acc[4 * e + 3] = fmaf(f, x[e].w, acc[4 * e + 3]);
+                }
+            }
+            if (i >= mine) continue;
+            const long long pr = (long long)u.tile * p.tm + r;
+            T* dst = out + ((u.row0 + pr / p.group) * n_q_heads + u.head * p.group + pr % p.group) * HD + piece * 4;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float* v = acc + 8 * e;
+                *reinterpret_cast<uint4*>(dst + 8 * e) = make_uint4(tc::pack_bf16x2(v[0], v[1]), tc::pack_bf16x2(v[2], v[3]),
+                                                                    tc::pack_bf16x2(v[4], v[5]), tc::pack_bf16x2(v[6], v[7]));
+            }
+        }
+        return;
+    }
     // the rows, four at a time a warp: their loads are under way together
-    constexpr int C = HD / 32, PIECES = HD / 4, RG = 4;
+    constexpr int C = HD / 32, RG = 4;
     for (int i0 = warp * RG; i0 < mine; i0 += kCombineThreads / 32 * RG) {
         float acc[RG][C] = {};
 #pragma unroll 2
         for (int k = 0; k < parts; ++k) {
-            const float* src = part_at(k) + (long long)row0 * HD;
+            const float* src = part_at(k) + (long long)row0 * HD + lane * C;
             float x[RG][C];
 #pragma unroll
             for (int j = 0; j < RG; ++j) {
-                const int i = min(i0 + j, mine - 1);
-                int at = lane * C;
-                if constexpr (kSwizzled) at = (((at >> 2) ^ ((row0 + i) & (PIECES - 1))) << 2) | (at & 3);
+                const float* at = src + min(i0 + j, mine - 1) * HD;
                 if constexpr (HD == 128) {
-                    const float4 v = *reinterpret_cast<const float4*>(src + i * HD + at);
+                    const float4 v = *reinterpret_cast<const float4*>(at);
                     x[j][0] = v.x, x[j][1] = v.y, x[j][2] = v.z, x[j][3] = v.w;
                 } else {
-                    const float2 v = *reinterpret_cast<const float2*>(src + i * HD + at);
+                    const float2 v = *reinterpret_cast<const float2*>(at);
                     x[j][0] = v.x, x[j][1] = v.y;
                 }
             }
@@ -138,7 +168,7 @@ inline Plan make_plan(const PagedArgs& a, int tm, int tk) {
     return p;
 }
 
-template <typename T, int HD, bool kSwizzled = false>
+template <typename T, int HD, bool kColumns = false>
 cudaError_t launch_combine(const Plan& p, const Cut* cuts, const float* partial, void* out, int n_q_heads, int ctas,
                            cudaStream_t stream) {
     if (ctas < 2 || p.whole) return cudaSuccess;
@@ -152,7 +182,7 @@ cudaError_t launch_combine(const Plan& p, const Cut* cuts, const float* partial,
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attend_paged_combine_kernel<T, HD, kSwizzled>, p, cuts, partial, static_cast<T*>(out), n_q_heads, ctas);
+    return cudaLaunchKernelEx(&cfg, attend_paged_combine_kernel<T, HD, kColumns>, p, cuts, partial, static_cast<T*>(out), n_q_heads, ctas);
 }
 
 }  // namespace paged
