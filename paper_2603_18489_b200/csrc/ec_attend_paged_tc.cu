@@ -14,8 +14,9 @@
 // 0 x NaN is NaN).  A row sees keys below its limit; a tile whose keys are below the lowest limit of a warp's rows needs no mask.
 // The roles go from unit to unit by themselves: the producer, which is ahead of the others, writes down what the next unit is
 // (four places, B_SEGFULL and B_SEGFREE), barriers and ring go on, and so the next unit's keys are on their way while this one's
-// rows are still written (@@).  A unit that a cut divides leaves its un-normalised rows in the workspace, columns by fours with
-// the row fastest, as the threads hold them, for the second launch to join.
+// rows are still written (us, barriers set up anew for each unit / like this: 4096 causal rows with 32 heads on 8 227 / 164;
+// chunks of 1100 to 1330 rows 215 / 206).  A unit that a cut divides leaves its un-normalised rows in the workspace, columns by
+// fours with the row fastest, as the threads hold them, for the second launch to join.
 #include "ec_paged.cuh"
 #include "ec_paged_combine.cuh"
 #include "ec_tc_ptx.cuh"
@@ -766,9 +767,17 @@ size_t attend_paged_tiles_workspace(const ec_paged_desc& d) {
     const int ctas = sm_count();
     return cuts_bytes(ctas) + (size_t)ctas * 2 * 2 * BM * (d.head_dim + 2) * 4;
 }
+// Up to sixteen packed rows the other kernel has less to do.  With more it takes the keys once for every sixteen, and is still
+// the faster one while that is little: a unit of this kernel costs 8 us to start and end, and a few of them leave most SMs idle.
+// (tile of 16 rows, kv head) pairs x room for keys (the lengths are not known here), us here / there: 46 k (8 x 300 rows of 300
+// keys) 20.6 / 14.0; 48 k (2 x 40 of 1000, 8 heads) 26.9 / 14.8; 46 k (34 of 768, 28 heads on 4) 30.3 / 13.9; 131 k (4 x 8 of 2048, 32 on 8)
+// 29.2 / 23.9; 262 k (20 of 4096, 32 heads) 33.6 / 29.5; 288 k (8 x 32 of 1500, 12 heads of 64) 27.1 / 29.6; 368 k (8 x 34 of 768, 28 on 4) 36.6 /
+// 41.1; 786 k (34 of 8192, 32 heads) 44.5 / 54.9.
+constexpr double kFewKeys = 270e3;
 bool attend_paged_tiles_supported(const ec_paged_desc& d, int max_rows) {
-    return d.dtype == EC_BF16 && (long long)max_rows * (d.n_q_heads / d.n_kv_heads) > 16 &&
-           (long long)d.n_pages * d.n_kv_heads <= 0x7fffffffll;
+    const long long rows = (long long)max_rows * (d.n_q_heads / d.n_kv_heads);
+    if (d.dtype != EC_BF16 || rows <= 16 || (long long)d.n_pages * d.n_kv_heads > 0x7fffffffll) return false;
+    return (double)((rows + 15) / 16) * d.batch * d.n_kv_heads * d.max_pages * d.page_size > kFewKeys;
 }
 cudaError_t launch_attend_paged_tiles(const PagedArgs& a, cudaStream_t stream) {
     return a.d.head_dim == 128 ? launch<128>(a, stream) : launch<64>(a, stream);

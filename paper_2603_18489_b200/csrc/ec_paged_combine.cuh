@@ -73,7 +73,8 @@ __global__ void __launch_bounds__(kCombineThreads) attend_paged_combine_kernel(c
     __syncthreads();
     if constexpr (kColumns) {
         // Eight rows and 64 columns a warp, a lane sixteen columns of a row: its four loads of a part are 128 contiguous bytes of
-        // eight lanes, its two stores a sector.  (A row a warp, as below: 32 lines a load, 256 rows over 4096 keys 59 us, @@.)
+        // eight lanes, its two stores a sector.  (A row a warp, as below: 32 lines a load, 256 rows over 4096 keys 59 us a
+        // call, 47 like this.)
         for (int item = warp; item < (mine + 7) / 8 * (HD / 64); item += kCombineThreads / 32) {
             const int i = item / (HD / 64) * 8 + (lane & 7), r = row0 + min(i, mine - 1), piece = item % (HD / 64) * 16 + (lane >> 3) * 4;
             const long long off = (((r >> 7) * (HD / 4) + piece) * 128 + (r & 127)) * 4;

@@ -8,12 +8,12 @@ import _serving as ref
 pytestmark = pytest.mark.gpu
 
 
-def setup(dtype, lens, rows, hq, hkv, d, ps, seed=0, spare=3, garbage=True, pad_rows=0, scale_q=1.0):
+def setup(dtype, lens, rows, hq, hkv, d, ps, seed=0, spare=3, garbage=True, pad_rows=0, scale_q=1.0, room=0):
     """Random pages in a random order; everything that no position of a sequence uses is NaN."""
     g = torch.Generator().manual_seed(seed)
     b = len(lens)
     per = [-(-n // ps) for n in lens]
-    n_pages, max_pages = sum(per) + spare, max(max(per), 1) + 1
+    n_pages, max_pages = sum(per) + spare, max(max(max(per), 1) + 1, -(-room // ps))   # room: positions of the table
     ids = torch.randperm(n_pages, generator=g)
     table = torch.full((b, max_pages), -1, dtype=torch.int32)
     k, v = (torch.full((n_pages, hkv, ps, d), float("nan") if garbage else 0.0) for _ in range(2))
@@ -47,11 +47,13 @@ def check(s, got, lens, rows, ps, mask, d, bf16, scale=None):
         at += n
 
 
-def run(dtype, lens, rows, hq, hkv, d, ps, mask, **kw):
+def run(dtype, lens, rows, hq, hkv, d, ps, mask, kernel=None, **kw):
     import paper_2603_18489_b200 as ec
 
     s = setup(dtype, lens, rows, hq, hkv, d, ps, **kw)
     desc = ec.make_paged_desc(len(lens), hq, hkv, d, dtype, ps, s["n_pages"], s["max_pages"], mask_block=mask)
+    if kernel:
+        assert ec.ec_attend_paged_kernel_name(desc, max(rows)) == kernel
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
     out = torch.full_like(s["q"], 7.0)
     ec.ec_attend_paged(desc, s["q"], s["offsets"], s["lens"], max(max(rows), 1), s["table"], s["k"], s["v"], out=out,
@@ -219,3 +221,77 @@ def test_a_pool_beyond_32_bit_offsets(rows):
     desc = ec.make_paged_desc(1, 4, hkv, d, BF, ps, n_pages, 4, mask_block=1)
     out = ec.ec_attend_paged(desc, s["q"], s["offsets"], s["lens"], rows, table, k, v)
     check(s, out, [450], [rows], ps, 1, d, True)
+
+
+TILES, ROWS = "attend_paged_tiles_kernel", "attend_paged_rows_kernel"
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("mask", [0, 1, 5, 32])
+@pytest.mark.parametrize("ps", [16, 32, 64, 128])
+def test_tiles_kernel(d, mask, ps):
+    """One and two row tiles, one key tile and many, empty sequences, ends inside a page and a tile; room that the lengths do not use."""
+    lens, rows = [1, 70, 257, 0, 640, 385, 128, 900], [1, 33, 257, 2, 100, 60, 128, 17]
+    run(BF, lens, rows, 6, 2, d, ps, mask, kernel=TILES, pad_rows=5, room=65536)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_tiles_kernel_second_pass(d):
+    """Scores that leave the first pass's range: the unit is done again with running maxima, for one row tile and for two."""
+    for mask in (0, 1):
+        run(BF, [700, 300], [40, 200], 4, 2, d, 32, mask, kernel=TILES, scale_q=60.0, room=65536)
+
+
+@pytest.mark.parametrize("hq,hkv,rows,kv", [(7, 1, 3, 4000), (1, 1, 200, 3000), (64, 2, 40, 700), (128, 1, 9, 300), (9, 9, 18, 2000)])
+def test_tiles_kernel_cuts_and_groups(hq, hkv, rows, kv):
+    run(BF, [kv, kv // 2 + 1], [rows, 1], hq, hkv, 128, 16, 1, kernel=TILES, room=1 << 18)
+
+
+@pytest.mark.parametrize("rows", [9, 16, 3])
+def test_rows_kernel_whole_and_cut(rows):
+    for room, lens in ((0, [500, 77, 1]), (8000, [2500, 77, 1])):
+        run(BF, lens, [min(rows, n) for n in lens], 1, 1, 128, 16, 1, kernel=ROWS, room=room)
+        run(BF, lens, [min(rows, n) for n in lens], 2, 2, 64, 32, 0, kernel=ROWS, room=room)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_batches(seed):
+    g = np.random.default_rng(seed)
+    hkv = int(g.choice([1, 2, 3]))
+    hq, d, ps = hkv * int(g.choice([1, 2, 5, 8])), int(g.choice([64, 128])), int(g.choice([16, 32, 64, 128]))
+    b = int(g.integers(1, 9))
+    lens = [int(x) for x in g.integers(0, 1 + int(g.choice([40, 500, 1500])), b)]
+    rows = [int(g.integers(0, min(n, int(g.choice([2, 40, 300]))) + 1)) for n in lens]
+    if sum(rows) == 0:
+        lens[0], rows[0] = 5, 1
+    run(BF if seed % 4 else F32, lens, rows, hq, hkv, d, ps, int(g.choice([0, 1, 7, 32])), room=int(g.choice([0, 0, 40000])), pad_rows=int(g.integers(0, 3)))
+
+
+def test_a_captured_call_serves_other_lengths_on_the_tiles_kernel():
+    import paper_2603_18489_b200 as ec
+
+    lens, rows = [2000, 1100, 300], [150, 40, 300]
+    s = setup(BF, lens, rows, 8, 2, 128, 64, garbage=False, room=16384)
+    desc = ec.make_paged_desc(3, 8, 2, 128, BF, 64, s["n_pages"], s["max_pages"], mask_block=1)
+    assert ec.ec_attend_paged_kernel_name(desc, 300) == TILES
+    ws = ec.new_workspace(ec.ec_attend_paged_workspace_bytes(desc, 300))
+    out = torch.empty_like(s["q"])
+
+    def call():
+        ec.ec_attend_paged(desc, s["q"], s["offsets"], s["lens"], 300, s["table"], s["k"], s["v"], out=out, workspace=ws)
+
+    call()
+    first = out.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, first)
+    lens = [151, 1100, 300]
+    s["lens"].copy_(torch.tensor(lens, dtype=torch.int32))
+    graph.replay()
+    torch.cuda.synchronize()
+    check(s, out, lens, rows, 64, 1, 128, True)
