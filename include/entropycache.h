@@ -293,7 +293,7 @@ ec_status ec_select_recent_sliding(int32_t *history, int32_t ctx_len, int32_t ba
  * page_table        int32 [batch, max_pages]: position p of sequence b stands in page page_table[b, p / page_size]
  * row_offsets       int32 [batch + 1], ascending: the new rows of sequence b are rows row_offsets[b] ..
  *                   row_offsets[b+1] - 1 of q, k, v and out, all [n_rows, heads, head_dim]; rows behind
- *                   row_offsets[batch] are padding: not read, left as they were
+ *                   row_offsets[batch] are padding: their values do not matter, they are left as they were
  * kv_lens           int32 [batch]: positions of the sequence, its new rows among them
  * All DEVICE pointers, read by the kernels: nothing about lengths is known on the host, so a captured call serves
  * every later step. */

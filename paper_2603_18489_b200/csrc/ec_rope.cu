@@ -17,18 +17,35 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxTokens = 8;   // rows a CTA, at most
 
-__device__ __forceinline__ void load8(const float* p, float* v) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-}
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float* v) {
-    const uint4 a = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+// 8 values as they are loaded
+template <typename T>
+struct Raw {
+    uint4 v[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = *(reinterpret_cast<const uint4*>(p) + i);
     }
+    __device__ __forceinline__ void values(float* x) const {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                x[4 * i] = __uint_as_float(v[i].x), x[4 * i + 1] = __uint_as_float(v[i].y), x[4 * i + 2] = __uint_as_float(v[i].z),
+                      x[4 * i + 3] = __uint_as_float(v[i].w);
+        } else {
+            const uint32_t w[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[2 * i] = __uint_as_float(w[i] << 16);
+                x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            }
+        }
+    }
+};
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float* x) {
+    Raw<T> r;
+    r.load(p);
+    r.values(x);
 }
 __device__ __forceinline__ void store8(float* p, const float* v) {
     *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
@@ -45,7 +62,7 @@ struct Row {       // what a CTA knows of one of its rows
 };
 
 template <typename T, int HD, bool kPaged>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs a, int tokens) {
+__global__ void __launch_bounds__(kThreads, 4) rope_kernel(const RopeArgs a, int tokens) {
     constexpr int LH = HD / 16, HPB = kThreads / LH;   // lanes of a head, heads at a time
     __shared__ float2 turn[kMaxTokens][HD / 2];        // cosine, sine
     __shared__ Row rows[kMaxTokens];
@@ -54,6 +71,28 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs a, int to
     const int half = a.d.rot_dim / 2;
     tc::pdl_wait();
     tc::pdl_launch_dependents();
+    const int hq = a.d.n_q_heads, hkv = a.d.n_kv_heads;
+    const int heads = hq + hkv * (kPaged ? 2 : 1);
+    const int l = tid % LH;
+    // this lane's two pieces of a head
+    const int pairs = a.d.rot_dim / 16;   // lanes that rotate
+    const bool inter = a.d.flags & EC_ROPE_INTERLEAVED, rotates = l < pairs;
+    const int c0 = rotates && !inter ? l : 2 * l, c1 = rotates && !inter ? l + pairs : 2 * l + 1;
+    const bool norm = a.q_weight != nullptr;
+    // The next head's loads are under way while this one is worked on, the first one's already under the angles.  (Two heads at a
+    // time take 80 registers instead of 56 and with them a CTA of each SM: 45 us instead of 39 for 8 x 1531 rows, 126 instead of 121.)
+    Raw<T> raw[2];
+    const auto ask = [&](int item) {
+        if (item >= n * heads) return;
+        const int t = item / heads, h = item - t * heads;
+        const long long r = r0 + t;
+        const T* src = h < hq ? static_cast<const T*>(a.q) + r * a.q_stride + (long long)h * HD
+                     : h < hq + hkv ? static_cast<const T*>(a.k) + r * a.k_stride + (long long)(h - hq) * HD
+                                    : static_cast<const T*>(a.v) + r * a.v_stride + (long long)(h - hq - hkv) * HD;
+        raw[0].load(src + c0 * 8);
+        raw[1].load(src + c1 * 8);
+    };
+    ask(tid / LH);
     for (int i = tid; i < n * half; i += kThreads) {
         const int t = i / half, f = i % half;
         const double turns = (double)a.positions[r0 + t] * (double)a.inv_freq[f] * 0.15915494309189533577;   // / (2 pi)
@@ -91,96 +130,65 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeArgs a, int to
     }
     __syncthreads();
 
-    const int hq = a.d.n_q_heads, hkv = a.d.n_kv_heads;
-    const int heads = hq + hkv * (kPaged ? 2 : 1);
-    const int l = tid % LH;
-    // this lane's two pieces of a head
-    const int pairs = a.d.rot_dim / 16;   // lanes that rotate
-    const bool inter = a.d.flags & EC_ROPE_INTERLEAVED, rotates = l < pairs;
-    const int c0 = rotates && !inter ? l : 2 * l, c1 = rotates && !inter ? l + pairs : 2 * l + 1;
-    const bool norm = a.q_weight != nullptr;
-    // kItems heads at a time: their loads are under way together
-    constexpr int kItems = 2;
-    for (int item0 = tid / LH; item0 < n * heads; item0 += kItems * HPB) {
-        float x[kItems][2][8];
-        T* dst[kItems];
-        int tok[kItems], kind[kItems];   // kind: 0 a query head, 1 a key head, 2 a value head
-#pragma unroll
-        for (int e = 0; e < kItems; ++e) {
-            const int item = item0 + e * HPB;
-            dst[e] = nullptr;
-            if (item >= n * heads) continue;
-            const int t = item / heads, h = item - t * heads;
-            const Row row = rows[t];
-            const long long r = r0 + t;
-            const T* src;
-            tok[e] = t;
-            if (h < hq) {
-                kind[e] = 0;
-                src = static_cast<const T*>(a.q) + r * a.q_stride + (long long)h * HD;
-                if (row.out) dst[e] = static_cast<T*>(a.q_out) + (r * hq + h) * HD;
-            } else if (h < hq + hkv) {
-                const int hk = h - hq;
-                kind[e] = 1;
-                src = static_cast<const T*>(a.k) + r * a.k_stride + (long long)hk * HD;
-                if constexpr (kPaged) {
-                    if (row.kv >= 0) dst[e] = static_cast<T*>(a.k_out) + row.kv + (long long)hk * a.page_size * HD;
-                } else if (row.out) {
-                    dst[e] = static_cast<T*>(a.k_out) + (r * hkv + hk) * HD;
-                }
-            } else {
-                const int hk = h - hq - hkv;
-                kind[e] = 2;
-                src = static_cast<const T*>(a.v) + r * a.v_stride + (long long)hk * HD;
-                if (row.kv >= 0) dst[e] = static_cast<T*>(a.v_pages) + row.kv + (long long)hk * a.page_size * HD;
+    for (int item = tid / LH; item < n * heads; item += HPB) {
+        float x[2][8];
+        raw[0].values(x[0]);
+        raw[1].values(x[1]);
+        ask(item + HPB);
+        const int t = item / heads, h = item - t * heads;
+        const Row row = rows[t];
+        const long long r = r0 + t;
+        T* dst = nullptr;
+        if (h < hq) {
+            if (row.out) dst = static_cast<T*>(a.q_out) + (r * hq + h) * HD;
+        } else if (h < hq + hkv) {
+            if constexpr (kPaged) {
+                if (row.kv >= 0) dst = static_cast<T*>(a.k_out) + row.kv + (long long)(h - hq) * a.page_size * HD;
+            } else if (row.out) {
+                dst = static_cast<T*>(a.k_out) + (r * hkv + h - hq) * HD;
             }
-            if (dst[e]) {   // (padding rows are not read)
-                load8(src + c0 * 8, x[e][0]);
-                load8(src + c1 * 8, x[e][1]);
-            }
+        } else if (row.kv >= 0) {
+            dst = static_cast<T*>(a.v_pages) + row.kv + (long long)(h - hq - hkv) * a.page_size * HD;
         }
+        if (!dst) continue;   // (the lanes of a head agree, so the reduction below stays whole within them)
+        if (h < hq + hkv) {
+            if (norm) {
+                float ss = 0.f;
 #pragma unroll
-        for (int e = 0; e < kItems; ++e) {
-            if (!dst[e]) continue;   // (the lanes of a head agree, so the reduction below stays whole within them)
-            if (kind[e] < 2) {
-                if (norm) {
-                    float ss = 0.f;
+                for (int i = 0; i < 8; ++i) ss = fmaf(x[0][i], x[0][i], fmaf(x[1][i], x[1][i], ss));
+                const uint32_t lanes = ((1u << LH) - 1u) << ((tid & 31) / LH * LH);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) ss = fmaf(x[e][0][i], x[e][0][i], fmaf(x[e][1][i], x[e][1][i], ss));
-                    const uint32_t lanes = ((1u << LH) - 1u) << ((tid & 31) / LH * LH);
+                for (int o = LH / 2; o; o >>= 1) ss += __shfl_xor_sync(lanes, ss, o);
+                const float inv = 1.f / sqrtf(ss * (1.f / HD) + a.d.eps);
+                const T* w = static_cast<const T*>(h < hq ? a.q_weight : a.k_weight);
+                float wv[2][8];
+                load8(w + c0 * 8, wv[0]);
+                load8(w + c1 * 8, wv[1]);
 #pragma unroll
-                    for (int o = LH / 2; o; o >>= 1) ss += __shfl_xor_sync(lanes, ss, o);
-                    const float inv = 1.f / sqrtf(ss * (1.f / HD) + a.d.eps);
-                    const T* w = static_cast<const T*>(kind[e] == 0 ? a.q_weight : a.k_weight);
-                    float wv[2][8];
-                    load8(w + c0 * 8, wv[0]);
-                    load8(w + c1 * 8, wv[1]);
+                for (int i = 0; i < 8; ++i) x[0][i] *= inv * wv[0][i], x[1][i] *= inv * wv[1][i];
+            }
+            if (rotates && !inter) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[e][0][i] *= inv * wv[0][i], x[e][1][i] *= inv * wv[1][i];
+                for (int i = 0; i < 8; ++i) {
+                    const float2 cs = turn[t][l * 8 + i];
+                    const float p = x[0][i], q = x[1][i];
+                    x[0][i] = fmaf(p, cs.x, -q * cs.y);
+                    x[1][i] = fmaf(q, cs.x, p * cs.y);
                 }
-                if (rotates && !inter) {
+            } else if (rotates) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float2 cs = turn[tok[e]][l * 8 + i];
-                        const float p = x[e][0][i], q = x[e][1][i];
-                        x[e][0][i] = fmaf(p, cs.x, -q * cs.y);
-                        x[e][1][i] = fmaf(q, cs.x, p * cs.y);
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 cs = turn[t][l * 8 + j * 4 + i];
+                        const float p = x[j][2 * i], q = x[j][2 * i + 1];
+                        x[j][2 * i] = fmaf(p, cs.x, -q * cs.y);
+                        x[j][2 * i + 1] = fmaf(q, cs.x, p * cs.y);
                     }
-                } else if (rotates) {
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float2 cs = turn[tok[e]][l * 8 + j * 4 + i];
-                            const float p = x[e][j][2 * i], q = x[e][j][2 * i + 1];
-                            x[e][j][2 * i] = fmaf(p, cs.x, -q * cs.y);
-                            x[e][j][2 * i + 1] = fmaf(q, cs.x, p * cs.y);
-                        }
-                }
             }
-            store8(dst[e] + c0 * 8, x[e][0]);
-            store8(dst[e] + c1 * 8, x[e][1]);
         }
+        store8(dst + c0 * 8, x[0]);
+        store8(dst + c1 * 8, x[1]);
     }
 }
 
