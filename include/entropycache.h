@@ -420,7 +420,8 @@ ec_status ec_pages_compact(const ec_pages_desc *desc, int32_t *page_table, int32
 
 /* Page copy_src[i] -> copy_dst[i] for i < min(*n_copies, copy_cap), in K and V of n_layers pools that stand layer_bytes
  * apart (n_copies NULL: copy_cap pairs).  page_bytes and layer_bytes are multiples of 16.  Pairs with an id
- * outside [0, n_pages) are skipped and set *dev_status to EC_ERR_PAGE.  No page may be both a source and a destination. */
+ * outside [0, n_pages) are skipped and set *dev_status to EC_ERR_PAGE.  Destinations are distinct, and no page
+ * is both a source and a destination. */
 ec_status ec_pages_copy(void *k_pages, void *v_pages, int64_t page_bytes, int32_t n_pages, int32_t n_layers,
                         int64_t layer_bytes, const int32_t *copy_src, const int32_t *copy_dst, int32_t copy_cap,
                         const int32_t *n_copies, int32_t *dev_status, void *stream);

@@ -566,7 +566,7 @@ PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (t.size(1) > 1 && t.stride(1) != 1) raise(PyExc_ValueError, "logits rows must be contiguous");
         const int32_t type = dtype_code(t), rows = (int32_t)t.size(0), vocab = int32(a[1]);
         if (vocab > t.size(1)) raise(PyExc_ValueError, "logits rows hold fewer than vocab columns");
-        const int64_t stride = rows > 1 ? t.stride(0) : (t.size(1) + 7) / 8 * 8;   // (of one row the stride is not used)
+        const int64_t stride = t.stride(0);
         const float *u = c.floats(a[2], "u", rows), *temp = c.floats(a[3], "temperature", rows, true);
         const int32_t* top_k = c.ints(a[4], "top_k", rows, true);
         const float *top_p = c.floats(a[5], "top_p", rows, true), *min_p = c.floats(a[6], "min_p", rows, true);
