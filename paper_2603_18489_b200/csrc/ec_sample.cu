@@ -527,14 +527,13 @@ private:
                            u64 kept_c, u64 kept_w) {
         u64 n = k > 0 && (uint32_t)k < live ? k : live, sum = all_w;
         Found f;
-        const float per_unit = (float)(1.0 / s.unit);
         if (at_k) {
             if (!find(true, k, at[0], head, front[0], n_list, f)) return false;
             sum = f.weight;
         }
         if (p < 1.f) {
             const u64 target = reach(p, sum);
-            if (!find(false, target, head ? around((float)target * per_unit, sure) : at[1], head, front[1], n_list, f)) return false;
+            if (!find_weight(target, at[1], head, front[1], n_list, f)) return false;
             if (f.count < n) n = f.count, sum = f.weight;
         }
         if (mp > 1.f) {
@@ -551,9 +550,15 @@ private:
         }
         if (floor_units && kept_c < n) n = kept_c, sum = kept_w;
         const u64 target = pass(u, sum);
-        if (!find(false, target, head ? around((float)target * per_unit, sure) : at[2], head, front[2], n_list, f)) return false;
+        if (!find_weight(target, at[2], head, front[2], n_list, f)) return false;
         answer(a, r, f, n, sum);
         return true;
+    }
+    // (with all tokens at hand, where the target itself says, and a wider place if need be)
+    __device__ bool find_weight(u64 target, const Place& place, bool head, u64 front, int n_list, Found& f) {
+        if (!head) return find(false, target, place, head, front, n_list, f);
+        const float v = (float)((double)target / s.unit);
+        return find(false, target, around(v, usual), head, front, n_list, f) || find(false, target, around(v, sure), head, front, n_list, f);
     }
     // search() among the list's tokens of the fine bins of `place`; in front of them stand `front` units of weight, or (head)
     // the list's own tokens of lower bins
@@ -933,15 +938,13 @@ cudaError_t launch_as(const SampleArgs& a, int c, int segment, cudaStream_t stre
     return cudaLaunchKernelEx(&cfg, sample_kernel<T, kResident>, a, segment);
 }
 
-// CTAs of a row, and whether a segment is kept in shared memory (one CTA an SM) or read again from L2 (two).  A CTA takes
-// 14 us and 0.8 us for each 1000 tokens, two on an SM 22 and 1.5; the CTAs that do not fit at once make whole further rounds
-// while these are few.  us, kept with 2 / 4 / 8 CTAs, read again with 2 / 4 / 8: 32 rows of 126464 in fp32 69 40 53, 69 47 46;
-// 256 rows of 152064 in bf16 (not kept with 2) - 300 460, 281 266 -; 128 of 32000 in bf16 49 74 150, 53 58 109; 64 of 126464 in
-// fp32 90 81 130, 90 76 97; 16 of 152064 in bf16 102 73 62, 102 80 71.
-double rounds_us(double ctas, double at_once, double us) {
-    const double r = ctas / at_once;
-    return us * (r <= 3. ? ceil(r) : r);
-}
+// CTAs of a row, and whether a segment is kept in shared memory (one CTA an SM) or read again from L2 (two).  Kept, a CTA takes
+// 14 us and 0.8 us for each 1000 tokens, and the CTAs that do not fit at once make whole further rounds while these are few.  Read
+// again, 14 and 1.05 alone on an SM, 22 and 1.5 in pairs; in a single round the slowest rows count, 18 and 2.1.  From 16384
+// columns on a row has two CTAs at least: what one does by itself is the longer part of a slow row.
+// us, kept with 2 / 4 / 8 CTAs, read again with 2 / 4 / 8: 32 rows of 126464 in fp32 69 40 53, 69 47 46; 256 rows of 152064 in bf16
+// (not kept with 2) - 300 460, 281 266 -; 128 of 126464 in bf16 120 115 192, 148 110 143; 128 of 32000 49 74 150, 53 58 109 (one
+// CTA 69, 78); 64 of 126464 in fp32 90 81 130, 90 76 97; 16 of 152064 in bf16 102 73 62, 102 80 71.
 template <typename T>
 cudaError_t launch(const SampleArgs& a, cudaStream_t stream) {
     const auto segment = [&](int c) { return ((a.vocab + c - 1) / c + 7) & ~7; };
@@ -949,15 +952,16 @@ cudaError_t launch(const SampleArgs& a, cudaStream_t stream) {
     int best_c = kMaxCluster;
     bool kept = false;
     double best = 1e30;
-    for (int c = 1; c <= kMaxCluster; c *= 2) {
+    for (int c = a.vocab < 16384 ? 1 : 2; c <= kMaxCluster; c *= 2) {
         const int seg = segment(c);
         if (seg > kSegment || (c > 1 && seg < 1024)) continue;
         const double ctas = (double)a.n_rows * c;
         if ((int)HIST_BYTES + (long long)seg * (int)sizeof(T) <= kMaxDynamic) {
-            const double us = rounds_us(ctas, sms, 14. + 8e-4 * seg);
+            const double rounds = ctas / sms, us = (14. + 8e-4 * seg) * (rounds <= 3. ? ceil(rounds) : rounds);
             if (us < best) best = us, best_c = c, kept = true;
         }
-        const double us = ctas <= sms ? 14. + 1.05e-3 * seg : rounds_us(ctas, 2. * sms, 22. + 1.5e-3 * seg);
+        const double once = 18. + 2.1e-3 * seg, more = ctas / (2. * sms) * (22. + 1.5e-3 * seg);
+        const double us = ctas <= sms ? 14. + 1.05e-3 * seg : once > more ? once : more;
         if (us < best) best = us, best_c = c, kept = false;
     }
     return kept ? launch_as<T, true>(a, best_c, segment(best_c), stream) : launch_as<T, false>(a, best_c, segment(best_c), stream);
