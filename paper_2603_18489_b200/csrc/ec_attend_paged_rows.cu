@@ -1,14 +1,16 @@
-// ec_attend_paged for few query rows a kv head (decoding: one row a sequence) in bf16, and for fp32: sixteen packed query
-// rows a tile, the keys split over warps that know nothing of one another until the end.
+// ec_attend_paged for few query rows a kv head (decoding: one row a sequence) in bf16, and for fp32: eight or sixteen packed
+// query rows a tile, the keys split over warps that know nothing of one another until the end.
 //
-// Bound by the K/V bytes.  A CTA's four warps take the key tiles of 64 keys, a warp sixteen of them: it loads its own
-// chunk of K and V (rows of one page; cp.async, three stages deep, zeros behind the sequence's end, so that
-// what an unfinished page holds is never multiplied), forms the scores, keeps its own running maximum and sum, and multiplies
-// into its own accumulators.  Nothing but the merge of the four at the end of a unit's keys needs the CTA together.
-//   bf16   mma.sync m16n8k16 (the sixteen rows are its M; tcgen05 has no shape below 64 rows, and this is far from
-//          bound by the tensor pipe), P rounded to bf16 for the second product as the dense kernels do
+// Bound by the K/V bytes.  A CTA's warps (four; eight or sixteen where sequences are short) take the key tiles, sixteen keys
+// each: a warp loads its own chunk of K and V (rows of one page; cp.async, three stages deep, zeros behind the sequence's end, so
+// that what an unfinished page holds is never multiplied), forms the scores, keeps its own running maximum and sum, and multiplies
+// into its own accumulators.  Nothing but the merge at the end of a unit's keys needs the CTA together.
+//   bf16   mma.sync m16n8k16 (tcgen05 has no shape below 64 rows, and this is far from bound by the tensor pipe: 7.5 % busy), P
+//          rounded to bf16 for the second product as the dense kernels do
 //   fp32   FMA units; a lane has one key and eight rows for the scores, HD / 32 columns of all rows for the output
-// The work is cut as ec_paged.cuh says; combine_kernel joins the units that a cut divided.
+// The work is cut as ec_paged.cuh says; attend_paged_combine_kernel joins the units that a cut divided.
+// 32 sequences of 526 to 7892 keys, 32 heads on 8: 94 us, 5.2 TB/s (the bytes alone 76); the rest is planning (3 us), the ends of
+// units (a merge of the warps, 1.5 us each) and the join.  One token over 768 keys: 10.7 us.
 #include "ec_paged.cuh"
 #include "ec_paged_combine.cuh"
 #include "ec_tc_ptx.cuh"

