@@ -295,3 +295,57 @@ def test_a_captured_call_serves_other_lengths_on_the_tiles_kernel():
     graph.replay()
     torch.cuda.synchronize()
     check(s, out, lens, rows, 64, 1, 128, True)
+
+
+@pytest.mark.parametrize("d,heads", [(64, 40), (128, 48)])
+@pytest.mark.parametrize("mask", [0, 1])
+def test_many_units_a_cta_some_of_them_done_twice(d, heads, mask):
+    """Each CTA goes through several units of one and two row tiles, one key tile and more; in every other sequence the scores
+    leave the first pass's range, so that units with and without a second pass follow one another."""
+    import paper_2603_18489_b200 as ec
+
+    lens, rows = [130, 20, 300, 257, 140, 1, 500, 129], [20, 20, 150, 257, 17, 1, 40, 129]
+    s = setup(BF, lens, rows, heads, heads, d, 32, room=65536)
+    at = 0
+    for b, n in enumerate(rows):
+        if b % 2 == 0:
+            s["q"][at:at + n] *= 60
+        at += n
+    desc = ec.make_paged_desc(8, heads, heads, d, BF, 32, s["n_pages"], s["max_pages"], mask_block=mask)
+    assert ec.ec_attend_paged_kernel_name(desc, max(rows)) == TILES
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = ec.ec_attend_paged(desc, s["q"], s["offsets"], s["lens"], max(rows), s["table"], s["k"], s["v"], dev_status=status)
+    assert int(status) == 0
+    check(s, out, lens, rows, 32, mask, d, True)
+
+
+@pytest.mark.parametrize("dtype,room", [(BF, 0), (BF, 1 << 20), (F32, 0)])
+def test_only_empty_sequences(dtype, room):
+    import paper_2603_18489_b200 as ec
+
+    s = setup(dtype, [40, 0, 7], [0, 0, 0], 40, 1, 64, 16, pad_rows=30, room=room)
+    desc = ec.make_paged_desc(3, 40, 1, 64, dtype, 16, s["n_pages"], s["max_pages"], mask_block=1)
+    out = torch.full_like(s["q"], 7.0)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ec.ec_attend_paged(desc, s["q"], s["offsets"], s["lens"], 30, s["table"], s["k"], s["v"], out=out, dev_status=status)
+    assert (out == 7.0).all() and int(status) == 0
+
+
+def test_the_largest_batch():
+    g = np.random.default_rng(0)
+    lens = [int(x) for x in g.integers(0, 40, 1024)]
+    run(BF, lens, [min(n, 1 + i % 2) for i, n in enumerate(lens)], 2, 1, 64, 16, 1)
+    run(BF, lens, [min(n, 1 + i % 19) for i, n in enumerate(lens)], 2, 1, 64, 16, 1, kernel=TILES, room=4096)
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_fewer_rows_than_the_offsets_say(rows):
+    """Offsets beyond the rows of q: the rows that are there are computed, the rest is refused."""
+    import paper_2603_18489_b200 as ec
+
+    s = setup(BF, [100, 90], [rows, rows], 2, 2, 64, 16, room=1 << 18)
+    desc = ec.make_paged_desc(2, 2, 2, 64, BF, 16, s["n_pages"], s["max_pages"], mask_block=0)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    want = ec.ec_attend_paged(desc, s["q"], s["offsets"], s["lens"], rows, s["table"], s["k"], s["v"])
+    out = ec.ec_attend_paged(desc, s["q"][:rows].contiguous(), s["offsets"], s["lens"], rows, s["table"], s["k"], s["v"], dev_status=status)
+    assert int(status) == 2 and torch.equal(out, want[:rows])

@@ -137,3 +137,44 @@ def test_frequencies():
     got = ec.ec_sample(row.repeat(n, 1), 8, u)["token"]
     share = torch.bincount(got.long(), minlength=8).double() / n
     assert (share - torch.softmax(row.double(), 0)).abs().max() <= 1.0 / n
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_the_largest_vocabulary(dtype):
+    v = 1 << 20
+    x, u = logits(3, v, dtype, seed=9, sigma=2.0)
+    x[2] = 0.25                     # equal logits: found by the index
+    run(x, u)
+    run(x, u, top_k=70000, top_p=0.7, min_p=1e-4)
+    run(x, u, top_p=0.3, temperature=0.5)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("v", [5, 1001, 20001])
+def test_what_stands_behind_the_vocabulary_is_not_read(dtype, v):
+    x, u = logits(5, v, dtype, pad=-v % 8 + 16)
+    x[:, v:] = float("nan")
+    run(x, u, vocab=v, top_p=0.9)
+    x[:, v:] = float("inf")
+    run(x, u, vocab=v, top_k=3)
+
+
+def test_clusters_of_equal_and_scattered_logits():
+    """Rows that the estimates cannot settle, and rows that they can, next to one another."""
+    g = torch.Generator().manual_seed(2)
+    x = torch.randn(12, 60000, generator=g)
+    x[0] = torch.where(torch.rand(60000, generator=g) < 0.5, 1.0, 0.0)            # two values
+    x[1] = (torch.randint(0, 5, (60000,), generator=g) * 0.01).float()            # five close ones
+    x[2, :50000] = 3.0
+    x[3] = torch.linspace(0, 1e-4, 60000)                                          # all but equal
+    x[4] = torch.linspace(-80, 0, 60000)
+    x[5] *= 1e-6
+    x[6] *= 1e4
+    x[7, 100:] = -1e30
+    u = torch.rand(12, generator=g).numpy().astype(np.float32)
+    for dtype in (F32, BF):
+        y = x.to(dtype).cuda()
+        run(y, u)
+        run(y, u, top_p=0.6)
+        run(y, u, top_k=30000, top_p=0.9)
+        run(y, u, top_k=30000, min_p=0.3, temperature=0.7)

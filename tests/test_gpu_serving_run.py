@@ -165,3 +165,59 @@ def test_paged_equals_dense(dtype, hq, hkv, d, n, L):
     tol = ref.attend_tolerance(want, mass, size, d, L, dtype == BF)
     assert (np.abs(f64(out) - want) <= tol).all()
     assert (np.abs(f64(out) - f64(dense)[0]) <= 2 * tol).all()
+
+
+def test_a_whole_step_captured():
+    """Rotation, attention, projection, sampling and the pages' growth in one graph, replayed: every step as when called."""
+    import paper_2603_18489_b200 as ec
+
+    torch.manual_seed(3)
+    hq, hkv, d, ps, slots = 4, 2, 64, 16, 3
+    lens0 = [20, 33, 7]
+
+    def fresh():
+        table, lens, refs = ec.new_pages(slots, 8, 24)
+        k, v = (torch.zeros(24, hkv, ps, d, dtype=BF, device="cuda") for _ in range(2))
+        return dict(table=table, lens=lens, refs=refs, k=k, v=v, new=dev(lens0), grow=torch.ones(slots, dtype=torch.int32, device="cuda"),
+                    cs=torch.empty(24, dtype=torch.int32, device="cuda"), cd=torch.empty(24, dtype=torch.int32, device="cuda"), n=dev([0]),
+                    token=torch.zeros(slots, dtype=torch.int32, device="cuda"), ws1=ec.new_workspace(ec.ec_pages_workspace_bytes(24)),
+                    status=dev([0]), prob=torch.zeros(slots, device="cuda"), kept=torch.zeros(slots, dtype=torch.int32, device="cuda"))
+
+    desc = ec.make_paged_desc(slots, hq, hkv, d, BF, ps, 24, 8, mask_block=1)
+    rope = ec.make_rope_desc(hq, hkv, d, BF, d)
+    freq = (10000.0 ** (-torch.arange(d // 2, dtype=torch.float64) / (d // 2))).float().cuda()
+    embed = torch.randn(512, (hq + 2 * hkv) * d, device="cuda").to(BF)
+    proj = (torch.randn(hq * d, 512, device="cuda") * 0.3).to(BF)
+    offsets, u = dev(np.arange(slots + 1)), torch.rand(slots, device="cuda")
+    top_p = torch.full((slots,), 0.9, device="cuda")
+    ws2 = ec.new_workspace(ec.ec_attend_paged_workspace_bytes(desc, 1))
+    ws3 = ec.new_workspace(ec.ec_sample_workspace_bytes(slots, 512))
+
+    def step(s):
+        s["pos"] = s["new"].clone()
+        s["new"].add_(s["grow"])
+        ec.ec_pages_reserve(s["table"], s["lens"], s["refs"], s["pos"], s["new"], ps, s["cs"], s["cd"], s["n"], workspace=s["ws1"], dev_status=s["status"])
+        ec.ec_pages_copy(s["k"], s["v"], s["cs"], s["cd"], s["n"], dev_status=s["status"])
+        qkv = embed[s["token"].long()]
+        q, k, v = (qkv[:, o * d:(o + h) * d].unflatten(1, (h, d)) for o, h in ((0, hq), (hq, hkv), (hq + hkv, hkv)))
+        qo = ec.ec_qk_norm_rope_paged(rope, desc, q, k, v, offsets, s["pos"], freq, s["table"], s["k"], s["v"], dev_status=s["status"])
+        out = ec.ec_attend_paged(desc, qo, offsets, s["lens"], 1, s["table"], s["k"], s["v"], workspace=ws2, dev_status=s["status"])
+        ec.ec_sample(out.flatten(1) @ proj, 512, u, top_p=top_p, token_out=s["token"], prob_out=s["prob"], kept_out=s["kept"], workspace=ws3)
+
+    a = fresh()
+    called = []
+    for _ in range(40):
+        step(a)
+        called.append(a["token"].tolist())
+    assert int(a["status"]) == 0 and len({tuple(t) for t in called}) > 5
+    b = fresh()
+    start = {n: t.clone() for n, t in b.items() if torch.is_tensor(t)}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(b)
+    for n, t in start.items():
+        b[n].copy_(t)
+    for i in range(40):
+        graph.replay()
+        assert b["token"].tolist() == called[i], i
+    assert int(b["status"]) == 0 and torch.equal(a["k"], b["k"]) and torch.equal(a["table"], b["table"])
