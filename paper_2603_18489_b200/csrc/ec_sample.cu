@@ -378,10 +378,10 @@ private:
     __device__ __forceinline__ int bin_of_count(uint32_t target) const { return bin_reaching<uint32_t>(sh.cum_c, target); }
     __device__ __forceinline__ int bin_of_estimate(float v) const { return min(bin_reaching<float>(sh.cum_e, v), kFine - 2); }
     // Around the place where the running weight is `v`.  A bin's estimate is off by a factor of e^(nats / 2) at most, and so is
-    // every running one: `sure`.  With many tokens the errors cancel: a quarter of it, and a bin to either side, nearly always
-    // hold the place; where equal logits fill the bins beside it, a tenth and no further bin.
-    enum Width { sure, usual, narrow };
-    __device__ __forceinline__ Place around(float v, Width width) const {
+    // every running one: `sure`.  Over many tokens the errors cancel, and a tenth of a bin nearly always holds the place: `narrow`,
+    // one bin or two (a few hundred tokens of a flat row, whose taking costs); where it does not, a quarter and a bin to either side.
+    enum Width { narrow, usual, sure };
+    __device__ __forceinline__ Place around(float v, int width) const {
         const float margin = (width == sure ? 0.55f : width == usual ? 0.25f : 0.1f) * s.nats + 2e-5f;
         const int more = width == narrow ? 0 : 1;
         return Place{max(bin_of_estimate(v * (1.f - margin)) - more, 0), min(bin_of_estimate(v * (1.f + margin)) + more, kFine - 2)};
@@ -436,7 +436,7 @@ private:
         if (mp > 0.f) v = fminf(v, sh.cum_e[min((int)fminf(-logf(fminf(mp, 1.f)) / s.nats, 1e6f), kFine - 2)]);
         const float vu = v * (float)u;
         Place at[3];   // of the k-th token, of top-p's last, of the one that u picks
-        const auto places = [&](Width width) {
+        const auto places = [&](int width) {
             at[0] = at_k ? Place{bk, bk} : Place{1, 0};
             at[1] = at_p ? around(vp, width) : Place{1, 0};
             at[2] = around(vu, width);
@@ -452,7 +452,14 @@ private:
         places(sure);
         const int top = at_k ? bk : max(at[1].hi, at[2].hi);
         const bool head = sh.cum_c[top] <= kList;
-        if (!head && !places(usual) && !places(narrow)) return false;
+        for (int width = head ? sure : narrow; width <= (head ? sure : usual); ++width) {
+            if (!head && !places(width)) return false;
+            if (collect(a, r, k, p, mp, u, floor_units, tiny, least_u, at, head, at_k, at_p, bk, top, live)) return true;
+        }
+        return false;
+    }
+    __device__ bool collect(const SampleArgs& a, int r, int k, float p, float mp, double u, u64 floor_units, bool tiny, double least_u,
+                            const Place (&at)[3], bool head, bool at_k, bool at_p, int bk, int top, uint32_t live) {
         // ---- the tokens, and the weights in front of them ----
         u64* list = reinterpret_cast<u64*>(hist);
         if (tid == 0) sh.n_list = 0;
