@@ -8,7 +8,7 @@
 //      weights, sums those in front of each place exactly and takes the tokens around it; one CTA settles the rest
 //      among these few thousand.  Rows with a top k whose prefix fits the list weigh nothing but that prefix;
 //   3  where equal logits (a constant row) or an estimate that was off leave that undone, weights by 16 bins and searches that
-//      narrow one bin down, at worst to single tokens: two rows in a thousand, and some 80 us each.
+//      narrow one bin down, at worst to single tokens: a few rows in a thousand, and some 80 us each.
 //
 // Weights are exp of fp64 arguments, rounded once to units of 2^-47 to 2^-43 of the largest weight (by the vocabulary alone,
 // see unit_bits_of) and summed as integers.  fp32 sums of 10^5 weights would be off by some 10^-7 of their total, as much as a
@@ -365,7 +365,8 @@ private:
     // which there are 1.4) give the place of the k-th token exactly, and, times the weight at a bin's middle, the places where
     // the running weight reaches what top-p and u ask for to within a fraction of a bin.  One more pass then forms all weights,
     // sums those in front of each place and takes the tokens of the bins around it; rank 0 finds the tokens among these, and sees
-    // from the exact sums whether they stand there.  Where all tokens up to the last place fit the list, it takes them all.
+    // from the exact sums whether they stand there.  Where a top k is given and all tokens up to the k-th fit the list, it takes
+    // them all, and no other weight is formed.
     struct Place {
         int lo, hi;   // fine bins; lo > hi: not asked for
     };
@@ -432,14 +433,23 @@ private:
             const float eb = bk ? sh.cum_e[bk - 1] : 0.f;
             v = eb + (sh.cum_e[bk] - eb) * (float)((uint32_t)k - before) / (float)(sh.cum_c[bk] - before);
         }
-        if (at_p) v = vp = v * fmaxf(p, 0.f);
-        if (mp > 0.f) v = fminf(v, sh.cum_e[min((int)fminf(-logf(fminf(mp, 1.f)) / s.nats, 1e6f), kFine - 2)]);
-        const float vu = v * (float)u;
+        // the kept sum lies in [v, v_most]: top-p keeps up to a token more than it asks for, min-p some part of a bin
+        float v_most = v;
+        if (at_p) {
+            vp = v * fmaxf(p, 0.f);
+            v_most = fminf(v, vp + exp2f(-1.4426950f * s.nats * fmaxf(bin_of_estimate(vp) - 1.f, 0.f)));
+            v = vp;
+        }
+        if (mp > 0.f) {
+            const int b = min((int)fminf(-logf(fminf(mp, 1.f)) / s.nats, 1e6f), kFine - 2);
+            v = fminf(v, b ? sh.cum_e[b - 1] : 0.f);
+            v_most = fminf(v_most, sh.cum_e[min(b + 1, kFine - 2)]);
+        }
         Place at[3];   // of the k-th token, of top-p's last, of the one that u picks
         const auto places = [&](int width) {
             at[0] = at_k ? Place{bk, bk} : Place{1, 0};
             at[1] = at_p ? around(vp, width) : Place{1, 0};
-            at[2] = around(vu, width);
+            at[2] = Place{around(v * (float)u, width).lo, around(v_most * (float)u, width).hi};
             // (each begins no later than the next, as it should: the sums in front of them are sums of classes)
             if (at_k && at_p) at[1].lo = min(at[1].lo, bk);
             at[2].lo = min(at[2].lo, at_p ? at[1].lo : at_k ? bk : at[2].lo);
@@ -449,17 +459,19 @@ private:
                 if (at[i].lo <= at[i].hi) n += sh.cum_c[at[i].hi] - (at[i].lo ? sh.cum_c[at[i].lo - 1] : 0);
             return n <= kList;
         };
-        places(sure);
-        const int top = at_k ? bk : max(at[1].hi, at[2].hi);
-        const bool head = sh.cum_c[top] <= kList;
-        for (int width = head ? sure : narrow; width <= (head ? sure : usual); ++width) {
-            if (!head && !places(width)) return false;
-            if (collect(a, r, k, p, mp, u, floor_units, tiny, least_u, at, head, at_k, at_p, bk, top, live)) return true;
+        // the k-th token's bin and all before it, where these fit: no other weight is asked for
+        const bool head = at_k && sh.cum_c[bk] <= kList;
+        // (the sum, in units of the largest weight, says over how many tokens the errors cancel: 20 times at 400)
+        int width = head ? sure : sh.cum_e[kFine - 2] >= 400.f ? narrow : usual;
+        if (!places(width)) width = narrow;
+        for (; width <= sure; ++width) {
+            if (!places(width) && !head) return false;
+            if (collect(a, r, k, p, mp, u, floor_units, tiny, least_u, at, head, at_k, at_p, bk, live)) return true;
         }
         return false;
     }
     __device__ bool collect(const SampleArgs& a, int r, int k, float p, float mp, double u, u64 floor_units, bool tiny, double least_u,
-                            const Place (&at)[3], bool head, bool at_k, bool at_p, int bk, int top, uint32_t live) {
+                            const Place (&at)[3], bool head, bool at_k, bool at_p, int bk, uint32_t live) {
         // ---- the tokens, and the weights in front of them ----
         u64* list = reinterpret_cast<u64*>(hist);
         if (tid == 0) sh.n_list = 0;
@@ -471,18 +483,18 @@ private:
             }
         };
         u64 all_w = 0, kept_c = 0, kept_w = 0, front[3] = {0, 0, 0};
-        if (head && at_k) {   // nothing but these matters
+        if (head) {   // nothing but these matters
             each8([&](const float(&x)[8], int i) {
                 uint32_t in = 0;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) in |= (uint32_t)(fine_of(s, x[j]) <= top) << j;
+                for (int j = 0; j < 8; ++j) in |= (uint32_t)(fine_of(s, x[j]) <= bk) << j;
                 take(x, i, in);
             });
         } else {
             // Classes of tokens: in front of u's place, from there to top-p's, from there to the k-th's, behind; a thread sums the
             // weights of each in a column of its own.  A token is taken up to the end of the last place that began.
-            const int lo0 = head ? 0 : at[2].lo, lo1 = head || !at_p ? lo0 : at[1].lo, lo2 = head || !at_k ? lo1 : bk;
-            const int hi0 = head ? top : at[2].hi, hi1 = head || !at_p ? hi0 : max(hi0, at[1].hi), hi2 = head || !at_k ? hi1 : max(hi1, bk);
+            const int lo0 = at[2].lo, lo1 = at_p ? at[1].lo : lo0, lo2 = at_k ? bk : lo1;
+            const int hi0 = at[2].hi, hi1 = at_p ? max(hi0, at[1].hi) : hi0, hi2 = at_k ? max(hi1, bk) : hi1;
             const uint32_t column = tc::s2u(hist) + kList * 8 + tid * 8;   // (behind the list)
 #pragma unroll
             for (int c = 0; c < 4; ++c) sts64(column + c * (kThreads * 8), 0);
@@ -554,7 +566,7 @@ private:
         }
         if (mp > 1.f) {
             kept_c = 1, kept_w = (u64)s.unit;   // nobody reaches it: the first token alone
-        } else if (floor_units && head && at_k) {   // (what min-p keeps beyond the k-th does not matter)
+        } else if (floor_units && head) {   // (what min-p keeps beyond the k-th does not matter)
             const u64* list = reinterpret_cast<const u64*>(hist);
             kept_c = kept_w = 0;
             for (int i = tid; i < n_list; i += kThreads) {
