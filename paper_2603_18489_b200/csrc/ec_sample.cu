@@ -20,7 +20,8 @@
 //
 // Bound by instructions: some 45 a token for a weight (ten of them 64-bit), 61 % of the issue slots in use, the bytes 3 % of
 // the peak.  Of a row without top k on four CTAs (126464 tokens in fp32, clocks): step 1 13 k, counts and places 12 k, weights and
-// taking 20 to 29 k, settling 11 to 25 k; with a top k of 200 48 k in all.  32 rows 43 us, 256 of 152064 in bf16 219 to 280.
+// taking 20 to 22 k, settling 11 to 20 k; with a top k of 200 48 k in all.  32 rows 38 to 43 us, 256 of 152064 in bf16 210 to 300
+// (both by the rows).
 #include "ec_common.cuh"
 #include "ec_tc_ptx.cuh"
 
