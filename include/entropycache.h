@@ -381,7 +381,7 @@ ec_status ec_qk_norm_rope_paged(const ec_rope_desc *desc, const ec_paged_desc *p
  * ceil(kv_lens[b] / page_size); the rest of a row is not read.  Every call is deterministic: pages are handed out lowest
  * id first, in the order (sequence, entry).  The calls move no K or V: they leave pairs (copy_src[i], copy_dst[i]),
  * i < *n_copies, for ec_pages_copy; entries behind are -1.  Sources and destinations of one call are disjoint.
- * batch <= EC_PAGED_MAX_BATCH. */
+ * batch <= EC_PAGED_MAX_BATCH, batch * max_pages < 2^31, n_pages <= 2^28 (EC_ERR_UNSUPPORTED beyond). */
 typedef struct {
     int32_t batch, max_pages, n_pages, page_size;   /* page_size: any >= 1 */
 } ec_pages_desc;

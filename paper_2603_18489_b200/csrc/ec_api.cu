@@ -399,7 +399,8 @@ size_t paged_ws(const ec_paged_desc& d, int max_rows) {
 ec_status check_pages(const ec_pages_desc* d, const int32_t* table, const int32_t* lens, const int32_t* refs) {
     if (!d || !table || !lens || !refs) return EC_ERR_NULL;
     if (d->batch < 1 || d->max_pages < 1 || d->n_pages < 1 || d->page_size < 1) return EC_ERR_SHAPE;
-    if (d->batch > EC_PAGED_MAX_BATCH || d->n_pages > (1 << 28) || (long long)d->max_pages * d->page_size > 0x7fffff00ll)
+    if (d->batch > EC_PAGED_MAX_BATCH || d->n_pages > (1 << 28) || (long long)d->max_pages * d->page_size > 0x7fffff00ll ||
+        (long long)d->batch * d->max_pages > 0x7fffffffll)   // what a call asks for is counted in 32 bits
         return EC_ERR_UNSUPPORTED;
     return all_aligned4(table, lens, refs) ? EC_OK : EC_ERR_ALIGN;
 }

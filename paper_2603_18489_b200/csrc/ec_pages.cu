@@ -37,7 +37,9 @@ __device__ __forceinline__ int scan(int v, int& total, int* shared /* [kWarps + 
     total = all;
     return (warp ? below : 0) + x - v;
 }
-__device__ __forceinline__ int pages_for(int len, int page_size) { return (len + page_size - 1) / page_size; }
+__device__ __forceinline__ int pages_for(int len, int page_size) {   // (no sum: a page may be as long as an int)
+    return len / page_size + (len % page_size != 0);
+}
 __device__ __forceinline__ int len_of(const ec_pages_desc& d, const int32_t* lens, int b) {
     return (int)min((long long)max(lens[b], 0), (long long)d.max_pages * d.page_size);
 }

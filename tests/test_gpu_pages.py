@@ -157,3 +157,22 @@ def test_a_pool_beyond_32_bit_offsets():
     k[3], v[3] = 1.0, 2.0
     ec.ec_pages_copy(k, v, dev([3]), dev([n - 1]))
     assert (k[n - 1] == 1).all() and (v[n - 1] == 2).all() and float(k.float().sum()) == 2 * 16 * 64
+
+
+@pytest.mark.parametrize("ps", [1, 2 ** 30, 2 ** 31 - 256])
+def test_pages_of_one_position_and_of_more_than_a_billion(ps):
+    import paper_2603_18489_b200 as ec
+
+    t, l, r = ec.new_pages(3, 8 if ps == 1 else 1, 9)
+    p = ref.Pages(t.cpu().numpy(), l.cpu().numpy(), r.cpu().numpy(), ps)
+    news = np.array([5, 0, 1] if ps == 1 else [ps, 0, 1000], np.int32)
+    cs, cd, n = lists(4)
+    ec.ec_pages_reserve(t, l, r, dev([0, 0, 0]), dev(news), ps, cs, cd, n)
+    assert p.reserve(np.zeros(3, np.int32), news, 4) == [] and n.item() == 0
+    same(t, l, r, p)
+    ec.ec_pages_fork(t, l, r, dev([2]), dev([1]), ps)
+    p.fork([2], [1])
+    same(t, l, r, p)
+    ec.ec_pages_release(t, l, r, dev([1, 1, 0]), ps)
+    p.release(np.array([1, 1, 0]))
+    same(t, l, r, p)

@@ -155,6 +155,10 @@ def test_pages_refuse(ec):
                           (pages_desc(4, 8, 20, 0), SHAPE), (pages_desc(1025, 8, 20, 16), UNSUPPORTED),
                           (pages_desc(4, 2 ** 28, 20, 16), UNSUPPORTED)):
             assert call(ctypes.byref(bad)) == code
+    # entries that 32 bits cannot count (reserve adds up what its sequences need)
+    many = pages_desc(1024, 2 ** 21, 20, 1)
+    for call in calls.values():
+        assert call(ctypes.byref(many)) == UNSUPPORTED
     g = ctypes.byref(good)
     assert calls["fork"](g, n=-1) == SHAPE and calls["fork"](g, n=5) == SHAPE and calls["fork"](g, n=0) == OK
     assert calls["reserve"](g, cap=-1) == SHAPE and calls["reserve"](g, size=79) == WORKSPACE and calls["reserve"](g, ws=ODD) == ALIGN
