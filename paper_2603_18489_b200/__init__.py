@@ -17,6 +17,7 @@ Functions carry the names of the C entry points declared in
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -315,6 +316,12 @@ def ec_select_recent_sliding(history, state, masked, decoded_flags, window: int,
 
 
 # ---- paged cache, rotation, sampling ---------------------------------------------------------------------------------
+def _room(stream):
+    """Where a call makes tensors of its own: they belong to the stream that the call runs on, so that their memory is not
+    filled, or used again, out of its order."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def _type_code(dtype) -> int:
     if isinstance(dtype, int):
         return dtype
@@ -362,9 +369,10 @@ def ec_attend_paged(desc: ec_paged_desc, q, row_offsets, kv_lens, max_rows: int,
     int32 [B], page_table int32 [B, max_pages] (read on the device); k_pages, v_pages [n_pages, H_kv, page_size, D].
     Returns `out` [n_rows, H_q, D]; rows behind row_offsets[B] are left as they were."""
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        with _room(stream):
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if workspace is None:
-        with torch.cuda.device(q.device):
+        with _room(stream), torch.cuda.device(q.device):
             workspace = new_workspace(ec_attend_paged_workspace_bytes(desc, max_rows), q.device)
     status = _native.attend_paged(desc, q, row_offsets, kv_lens, max_rows, page_table, k_pages, v_pages, out, workspace,
                                   dev_status, stream)
@@ -378,10 +386,11 @@ def ec_qk_norm_rope(desc: ec_rope_desc, q, k, positions, inv_freq, q_weight=None
     """Norms of the query and key heads (if weights are given) and the position rotation in one pass.  q [..., H_q, D], k
     [..., H_kv, D]: rows may be slices of a packed projection; positions int32, one a row; inv_freq fp32 [rot_dim / 2].
     Returns (q_out, k_out), dense."""
-    if q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if k_out is None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    with _room(stream):
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if k_out is None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
     status = _native.qk_norm_rope(desc, q, k, q_weight, k_weight, positions, inv_freq, q_out, k_out, stream)
     if status:
         raise EcError(status, "ec_qk_norm_rope")
@@ -393,7 +402,8 @@ def ec_qk_norm_rope_paged(desc: ec_rope_desc, paged: ec_paged_desc, q, k, v, row
                           stream=None) -> torch.Tensor:
     """ec_qk_norm_rope with K, and V as it is, going into the pages at the rows' positions.  Returns q_out, dense."""
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        with _room(stream):
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     status = _native.qk_norm_rope_paged(desc, paged, q, k, v, q_weight, k_weight, row_offsets, positions, inv_freq, page_table,
                                         q_out, k_pages, v_pages, dev_status, stream)
     if status:
@@ -406,14 +416,15 @@ def ec_sample(logits, vocab: int, u, temperature=None, top_k=None, top_p=None, m
     """One token per logits row [R, row_stride] from the uniform numbers u fp32 [R]; temperature, top_p, min_p fp32 [R]
     and top_k int32 [R], each may be None.  Outputs are device tensors; nothing is synchronised."""
     rows, device = logits.shape[0], logits.device
-    if token_out is None:
-        token_out = torch.empty(rows, dtype=torch.int32, device=device)
-    if prob_out is None:
-        prob_out = torch.empty(rows, dtype=torch.float32, device=device)
-    if kept_out is None:
-        kept_out = torch.empty(rows, dtype=torch.int32, device=device)
-    if workspace is None:
-        workspace = new_workspace(ec_sample_workspace_bytes(rows, vocab), device)
+    with _room(stream):
+        if token_out is None:
+            token_out = torch.empty(rows, dtype=torch.int32, device=device)
+        if prob_out is None:
+            prob_out = torch.empty(rows, dtype=torch.float32, device=device)
+        if kept_out is None:
+            kept_out = torch.empty(rows, dtype=torch.int32, device=device)
+        if workspace is None:
+            workspace = new_workspace(ec_sample_workspace_bytes(rows, vocab), device)
     status = _native.sample(logits, vocab, u, temperature, top_k, top_p, min_p, token_out, prob_out, kept_out, workspace, stream)
     if status:
         raise EcError(status, "ec_sample")
@@ -438,7 +449,8 @@ def ec_pages_reserve(page_table, kv_lens, ref_counts, write_from, new_lens, page
     """Before positions write_from[b] .. new_lens[b] - 1 are written: missing pages are taken, shared ones replaced.  The
     pairs (copy_src[i], copy_dst[i]), i < n_copies, are for ec_pages_copy."""
     if workspace is None:
-        workspace = new_workspace(ec_pages_workspace_bytes(ref_counts.numel()), page_table.device)
+        with _room(stream):
+            workspace = new_workspace(ec_pages_workspace_bytes(ref_counts.numel()), page_table.device)
     status = _native.pages_reserve(page_table, kv_lens, ref_counts, page_size, write_from, new_lens, copy_src, copy_dst, n_copies,
                                    workspace, dev_status, stream)
     if status:
@@ -456,7 +468,8 @@ def ec_pages_compact(page_table, kv_lens, ref_counts, page_size: int, copy_src, 
                      stream=None) -> None:
     """Moves the pages in use to the lowest ids; the pairs to copy go to copy_src, copy_dst (n_pages / 2 long at least)."""
     if workspace is None:
-        workspace = new_workspace(ec_pages_workspace_bytes(ref_counts.numel()), page_table.device)
+        with _room(stream):
+            workspace = new_workspace(ec_pages_workspace_bytes(ref_counts.numel()), page_table.device)
     status = _native.pages_compact(page_table, kv_lens, ref_counts, page_size, copy_src, copy_dst, n_copies, workspace, stream)
     if status:
         raise EcError(status, "ec_pages_compact")

@@ -221,3 +221,37 @@ def test_a_whole_step_captured():
         graph.replay()
         assert b["token"].tolist() == called[i], i
     assert int(b["status"]) == 0 and torch.equal(a["k"], b["k"]) and torch.equal(a["table"], b["table"])
+
+
+def test_what_a_call_makes_belongs_to_its_stream(monkeypatch):
+    """Outputs and workspaces that are not given are made on the stream that is: a fill on another one, or another's use of the
+    memory once the call has returned, would run beside its kernels."""
+    import paper_2603_18489_b200 as ec
+
+    p = Program()
+    q = torch.randn(3, p.hq, p.d, dtype=BF, device="cuda")
+    k, v = (torch.randn(3, p.hkv, p.d, dtype=BF, device="cuda") for _ in range(2))
+    ro, pos, none, lens = dev([0, 2, 2, 3, 3, 3]), dev([0, 1, 0]), dev([0] * 5), dev([2, 0, 1, 0, 0])
+    x, u = torch.randn(4, 512, device="cuda"), torch.rand(4, device="cuda")
+    p.k.zero_(), p.v.zero_()
+
+    def step(stream):
+        ec.ec_pages_reserve(p.table, p.lens, p.refs, none, lens, p.ps, *p.lists, stream=stream)
+        a, b = ec.ec_qk_norm_rope(p.rope, q, k, pos, p.freq, stream=stream)
+        c = ec.ec_qk_norm_rope_paged(p.rope, p.paged, q, k, v, ro, pos, p.freq, p.table, p.k[0], p.v[0], stream=stream)
+        o = ec.ec_attend_paged(p.paged, c, ro, p.lens, 2, p.table, p.k[0], p.v[0], stream=stream)
+        s = ec.ec_sample(x, 512, u, stream=stream)
+        ec.ec_pages_compact(p.table, p.lens, p.refs, p.ps, *p.lists, stream=stream)
+        return a, b, c, o, s["token"], s["prob"], s["kept"]
+
+    want = step(None)
+    torch.cuda.synchronize()
+    side, made = torch.cuda.Stream(), []
+    for name in ("empty", "empty_like", "zeros"):
+        was = getattr(torch, name)
+        monkeypatch.setattr(torch, name, lambda *a, was=was, **kw: (made.append(torch.cuda.current_stream()), was(*a, **kw))[1])
+    got = step(side)
+    monkeypatch.undo()
+    side.synchronize()
+    assert len(made) == 11 and all(s == side for s in made)     # 7 outputs, workspaces of four calls
+    assert all(torch.equal(g, w) for g, w in zip(got, want))
