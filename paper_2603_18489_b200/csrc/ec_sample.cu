@@ -242,7 +242,8 @@ public:
         best = ~0ull, low64 = 0;
         for (int k = 0; k < n_ranks; ++k) best = min(best, in[k][64]), low64 = max(low64, in[k][65]);
         const float t = a.temperature ? a.temperature[r] : 1.f;
-        if (best == ~0ull || !(t > 0.f)) {
+        // (beside an infinite logit no other one weighs anything)
+        if (best == ~0ull || !(t > 0.f) || (uint32_t)(best >> 32) == order_of(INFINITY)) {
             if (rank == 0 && tid == 0) {
                 const bool some = best != ~0ull;
                 a.token_out[r] = some ? (int)(uint32_t)best : -1;

@@ -178,3 +178,27 @@ def test_clusters_of_equal_and_scattered_logits():
         run(y, u, top_p=0.6)
         run(y, u, top_k=30000, top_p=0.9)
         run(y, u, top_k=30000, min_p=0.3, temperature=0.7)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("v", [24, 20008, 200000])
+def test_rows_with_nan_and_infinities(dtype, v):
+    """NaN counts as -inf; a row with +inf gives the first such token, for certain."""
+    import paper_2603_18489_b200 as ec
+
+    x, u = logits(6, v, dtype, seed=4, sigma=2.0)
+    x[0, ::3] = float("nan")
+    x[1] = float("nan")
+    x[2, 1:] = float("nan")
+    x[3, 5::7] = float("inf")
+    x[4, ::2] = float("nan")
+    x[4, 9] = float("inf")
+    x[5] = float("-inf")
+    plain = torch.where(torch.isnan(x), torch.full_like(x, float("-inf")), x)
+    ut = torch.tensor(u, device="cuda")
+    for kw in ({}, dict(top_p=0.7), dict(top_k=7), dict(top_k=v // 2, top_p=0.9, min_p=0.01), dict(min_p=0.3), dict(temperature=0.0)):
+        t = {k: torch.full((6,), z, device="cuda", dtype=torch.int32 if k == "top_k" else F32) for k, z in kw.items()}
+        got, same = ec.ec_sample(x, v, ut, **t), ec.ec_sample(plain, v, ut, **t)
+        assert all(torch.equal(got[k], same[k]) for k in got), kw
+        assert got["token"].tolist()[1:] == [-1, 0, 5, 9, -1] and got["kept"].tolist()[1:] == [0, 1, 1, 1, 0], kw
+        assert got["prob"].tolist()[1:] == [0, 1, 1, 1, 0] and got["token"][0].item() % 3 != 0, kw
