@@ -237,6 +237,7 @@ public:
         });
         u64 low64 = low;
         block_min_max(best, low64);
+        tc::cluster_wait();   // (the row's other CTAs have started: their shared memory may be written)
         publish(64, best), publish(65, low64);
         const u64(*in)[72] = exchange();
         best = ~0ull, low64 = 0;
@@ -935,6 +936,7 @@ __global__ void __launch_bounds__(kThreads, kResident ? 1 : 2) sample_kernel(con
     extern __shared__ __align__(16) unsigned char hist[];   // the bins (or lists), then the segment
     __shared__ Shared sh;
     cg::cluster_group cluster = cg::this_cluster();
+    tc::cluster_arrive_relaxed();   // "this CTA has started"; run() waits for the others' behind the first pass over the row
     for (int i = threadIdx.x; i < 64 * 16; i += kThreads) sh.tab.v[i >> 4][i & 15] = exp2((double)(i >> 4) / 64.0);
     tc::pdl_wait();
     tc::pdl_launch_dependents();
