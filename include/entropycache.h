@@ -445,7 +445,7 @@ size_t ec_sample_workspace_bytes(int32_t n_rows, int32_t vocab);
  * -inf.  A row without a token gives token -1, prob 0, kept 0.  logits: [n_rows, row_stride_elems] of `dtype`, the first
  * `vocab` columns are read.  temperature, top_p, min_p fp32 [n_rows], top_k int32 [n_rows]:
  * each may be NULL (1, off, off, off).  u fp32 [n_rows], in [0, 1).  Weights are formed in 64 bits and summed as
- * integers in units of 2^-43 of the largest or finer (2^-47 up to 32768 columns, 2^-45 at 126464), so results do not
+ * integers in units of 2^-43 of the largest or finer (2^-47 up to 28672 columns, 2^-45 at 126464), so results do not
  * depend on how the work is split.  prob_out and kept_out may
  * be NULL.  vocab <= 1048576.  All DEVICE pointers; rows 16-byte aligned as for ec_entropy_gate. */
 ec_status ec_sample(const void *logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t row_stride_elems,

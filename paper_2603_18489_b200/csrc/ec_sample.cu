@@ -47,10 +47,10 @@ constexpr int kFew = 128;                  // candidates that are ranked against
 constexpr uint32_t HIST_BYTES = kBins * kThreads * 8;
 constexpr int kMaxDynamic = 232448 - 34816;   // (the rest: struct Shared)
 constexpr int kMaxUnitBits = 47;
-// a thread's weights, none above one, have to fit kWeightBits: as fine a unit as the whole row on one CTA leaves room for
+// a thread's weights, none above one, have to stay below 2^kWeightBits: as fine a unit as the whole row on one CTA leaves room for
 __host__ __device__ constexpr int unit_bits_of(int vocab) {
     int bits = kMaxUnitBits;
-    while (bits > 43 && (long long)((vocab + 4095) / 4096 * 8) << bits > 1ll << kWeightBits) --bits;
+    while (bits > 43 && (long long)((vocab + 4095) / 4096 * 8) << bits >= 1ll << kWeightBits) --bits;
     return bits;
 }
 constexpr int kFine = 1024;                // fine bins: counts alone; the last: weights that round to 0
