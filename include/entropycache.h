@@ -441,8 +441,8 @@ size_t ec_sample_workspace_bytes(int32_t n_rows, int32_t vocab);
  *     kept_out  = n = min(n_k, n_p, n_m)
  *     token_out = the first of the n whose running sum of w exceeds u * S, S = their sum; the n-th if none does
  *     prob_out  = w[token] / S
- * temperature <= 0 decodes greedily (token = argmax, prob = 1, kept = 1), and so does a row with a logit of +inf.  NaN counts as
- * -inf.  A row without a token gives token -1, prob 0, kept 0.  logits: [n_rows, row_stride_elems] of `dtype`, the first
+ * temperature <= 0 decodes greedily (token = argmax, prob = 1, kept = 1), and so does a row with a logit of +inf; a temperature
+ * between 0 and 2^-126 counts as 2^-126.  A logit of NaN counts as -inf.  A row without a token gives token -1, prob 0, kept 0.  logits: [n_rows, row_stride_elems] of `dtype`, the first
  * `vocab` columns are read.  temperature, top_p, min_p fp32 [n_rows], top_k int32 [n_rows]:
  * each may be NULL (1, off, off, off).  u fp32 [n_rows], in [0, 1).  Weights are formed in 64 bits and summed as
  * integers in units of 2^-43 of the largest or finer (2^-47 up to 28672 columns, 2^-45 at 126464), so results do not

@@ -242,7 +242,7 @@ public:
         const u64(*in)[72] = exchange();
         best = ~0ull, low64 = 0;
         for (int k = 0; k < n_ranks; ++k) best = min(best, in[k][64]), low64 = max(low64, in[k][65]);
-        const float t = a.temperature ? a.temperature[r] : 1.f;
+        float t = a.temperature ? a.temperature[r] : 1.f;
         // (beside an infinite logit no other one weighs anything)
         if (best == ~0ull || !(t > 0.f) || (uint32_t)(best >> 32) == order_of(INFINITY)) {
             if (rank == 0 && tid == 0) {
@@ -253,6 +253,9 @@ public:
             }
             return;
         }
+        // (Below 2^-126 it counts as that: per_bin and per_fine are finite, so a row of logits within 10^-36 of one another stays in
+        // the first bins however far a smaller t spreads its weights, and their exponents, over 2^1022, would wrap.)
+        t = fmaxf(t, 1.17549435e-38f);
         s.top = value_of((uint32_t)(best >> 32));
         s.c = 64.0 * 1.4426950408889634074 / (double)t;
         s.table = tc::s2u(&sh.tab.v[0][tid & 15]);
@@ -574,7 +577,7 @@ private:
             kept_c = kept_w = 0;
             for (int i = tid; i < n_list; i += kThreads) {
                 const float x = value_of((uint32_t)(list[i] >> 32));
-                const u64 units = weight_units(s, x);
+                const u64 units = weight_units(s, fmaxf(x, s.low));
                 if (tiny ? ((double)x - s.wide_top) * s.c >= least_u : units >= floor_units) kept_c += 1, kept_w += units;
             }
             block_sum(kept_c, kept_w);
