@@ -45,7 +45,7 @@ void* dev(PyObject* o, const char* name) {
 template <class T>
 T* dev_as(PyObject* o, const char* name) { return static_cast<T*>(dev(o, name)); }
 
-size_t bytes_of(PyObject* o) { return o == Py_None ? 0 : THPVariable_Unpack(o).nbytes(); }
+size_t bytes_of(PyObject* o) { return o == Py_None ? 0 : tensor(o, "workspace").nbytes(); }
 
 int32_t dtype_code(const at::Tensor& t) {
     if (t.scalar_type() == at::kFloat) return EC_F32;
