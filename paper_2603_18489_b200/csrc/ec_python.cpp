@@ -434,20 +434,23 @@ public:
         if (!t.is_contiguous()) raise(PyExc_ValueError, "workspace must be contiguous");
         return t.data_ptr();
     }
-    // [rows, heads, dim] whose heads are contiguous; rows may be apart.  Returns the pointer, sets the stride.
+    // [..., heads, dim] whose heads are contiguous and whose rows are one stride apart, as in a slice of a packed projection.
+    // Returns the pointer, sets the stride.
     void* rows(PyObject* o, const char* name, at::ScalarType type, int64_t n_rows, int64_t heads, int64_t dim, int64_t* stride) {
         const at::Tensor& t = cuda(o, name);
         if (t.scalar_type() != type) raise(PyExc_TypeError, std::string(name) + " must be " + c10::toString(type));
         const int64_t d = t.dim();
-        if (d < 3 || t.size(d - 1) != dim || t.size(d - 2) != heads) raise(PyExc_ValueError, std::string(name) + " must be [rows, heads, head_dim]");
+        if (d < 3 || t.size(d - 1) != dim || t.size(d - 2) != heads) raise(PyExc_ValueError, std::string(name) + " must be [..., heads, head_dim]");
         if (t.numel() != n_rows * heads * dim) raise(PyExc_ValueError, std::string(name) + " must have one row for each row of q");
         if ((dim > 1 && t.stride(d - 1) != 1) || (heads > 1 && t.stride(d - 2) != dim))
             raise(PyExc_ValueError, std::string("the heads of a row of ") + name + " must be contiguous");
         *stride = heads * dim;
-        if (d == 3) {
-            if (t.size(0) > 1) *stride = t.stride(0);
-        } else if (!t.is_contiguous()) {
-            raise(PyExc_ValueError, std::string(name) + " must be contiguous or [rows, heads, head_dim]");
+        int64_t next = -1;   // the stride that makes a dimension one with those behind it
+        for (int64_t i = d - 3; i >= 0 && t.numel() > 0; --i) {
+            if (t.size(i) == 1) continue;
+            if (next < 0) *stride = t.stride(i);
+            else if (t.stride(i) != next) raise(PyExc_ValueError, std::string("the rows of ") + name + " must be one stride apart");
+            next = t.stride(i) * t.size(i);
         }
         return t.data_ptr();
     }
