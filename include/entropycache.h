@@ -323,7 +323,10 @@ size_t ec_attend_paged_workspace_bytes(const ec_paged_desc *desc, int32_t max_ro
  *                      block of m positions see the whole block and what stands before it)
  *     out[r, hq, :] = sum_{j < lim} softmax_j( scale * <q[r, hq, :], K[b, hq/g, j, :]> ) * V[b, hq/g, j, :]
  * A row that sees nothing gets zeros.  What the pages hold at positions from kv_lens[b] on is never used, NaN and
- * infinities there included; at the positions before it K and V must be finite.  fp32 accumulation, one rounding.
+ * infinities there included; at the positions before it K and V must be finite.  Scores, maxima and sums are fp32.  fp32
+ * inputs: the output is rounded once.  bf16 inputs: the weights exp(score - reference) are rounded to bf16 for their product
+ * with V, as ec_attend does (the tensor cores take both operands in one type), and the output once more: each by 2^-8 of
+ * itself at most.
  * n_rows: rows of q and out; max_rows: a bound of the rows of any one sequence (>= 1).  A sequence with more has only
  * its first max_rows rows computed, and one with kv_lens[b] outside [0, max_pages * page_size] is cut to that range;
  * both set *dev_status to EC_ERR_SHAPE.  A page id outside [0, n_pages) that a row would read sets it to EC_ERR_PAGE

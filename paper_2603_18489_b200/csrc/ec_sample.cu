@@ -18,8 +18,8 @@
 // A row is shared by a cluster of 1 to 8 CTAs, each with a contiguous segment of it.  In step 3 a thread has a column of its own
 // in the bins (16 x 512 x 8 bytes, no atomics, no bank conflicts): weight sum in the low 53 bits, count in the top 11.
 //
-// Bound by instructions: some 45 a token for a weight (ten of them 64-bit), 61 % of the issue slots in use, the bytes 3 % of
-// the peak.  Of a row without top k on four CTAs (126464 tokens in fp32, clocks): step 1 13 k, counts and places 12 k, weights and
+// Bound by instructions: some 45 a token for a weight (ten of them 64-bit).  256 x 152064 in bf16, two CTAs a row: 58 % of the issue
+// slots of an SM while it works, 28 % over the launch, which the slowest rows end; the bytes 4 % of the peak.  Of a row without top k on four CTAs (126464 tokens in fp32, clocks): step 1 13 k, counts and places 12 k, weights and
 // taking 20 to 22 k, settling 11 to 20 k; with a top k of 200 48 k in all.  32 rows 38 to 43 us, 256 of 152064 in bf16 210 to 300
 // (both by the rows).
 #include "ec_common.cuh"
