@@ -447,7 +447,7 @@ size_t ec_sample_workspace_bytes(int32_t n_rows, int32_t vocab);
  * temperature <= 0 decodes greedily (token = argmax, prob = 1, kept = 1), and so does a row with a logit of +inf; a temperature
  * between 0 and 2^-126 counts as 2^-126.  A logit of NaN counts as -inf.  A row without a token gives token -1, prob 0, kept 0.  logits: [n_rows, row_stride_elems] of `dtype`, the first
  * `vocab` columns are read.  temperature, top_p, min_p fp32 [n_rows], top_k int32 [n_rows]:
- * each may be NULL (1, off, off, off).  u fp32 [n_rows], in [0, 1).  Weights are formed in 64 bits and summed as
+ * each may be NULL (1, off, off, off).  u fp32 [n_rows], in [0, 1).  min_p compares in 64 bits.  Weights are formed in 64 bits and summed as
  * integers in units of 2^-43 of the largest or finer (2^-47 up to 28672 columns, 2^-45 at 126464), so results do not
  * depend on how the work is split.  prob_out and kept_out may
  * be NULL.  vocab <= 1048576.  All DEVICE pointers; rows 16-byte aligned as for ec_entropy_gate. */

@@ -272,12 +272,11 @@ public:
         const float p = a.top_p ? a.top_p[r] : 1.f;
         const double u = (double)a.u[r];
         const float mp = a.min_p ? a.min_p[r] : 0.f;
-        // (at least the largest stays; a bound below a unit asks the exponents instead of the weights)
-        const u64 floor_units = mp > 0.f ? (u64)fmin(ceil((double)mp * s.unit), s.unit) : 0;
-        const bool tiny = floor_units == 1;
-        const double least_u = tiny ? 64.0 * log2((double)mp) : 0.0;
+        // What min-p keeps, as a bound of the logit: w >= min_p where x >= top + t ln(min_p), formed in 64 bits (weights in units
+        // would tell min_p = 1e-13 apart to 4 %).  The 2^-54 stands for weights that are 1 in 64 bits.  The largest always stays.
+        const float least = mp > 0.f ? __double2float_ru(s.wide_top + (double)t * (log((double)mp) - 5.6e-17)) : 0.f;
         constexpr u64 kOne = 1ull << kWeightBits;
-        if (by_estimate(a, r, k, p, mp, u, floor_units, tiny, least_u)) return;
+        if (by_estimate(a, r, k, p, mp, u, least)) return;
 
         // ---- what the estimates could not settle: weights by bin, and searches that narrow a bin down ----
         const uint32_t column = tc::s2u(hist) + tid * 8;
@@ -299,13 +298,13 @@ public:
                     bump(column, b, add);
                     if constexpr (decltype(with_floor)::value) {
                         const u64 units = add & (kOne - 1);
-                        const bool in = add && (tiny ? ((double)x[j] - s.wide_top) * s.c >= least_u : units >= floor_units);
+                        const bool in = add && x[j] >= least;
                         kept_c += in, kept_w += in ? units : 0;
                     }
                 }
             });
         };
-        if (floor_units) weigh(std::true_type{});
+        if (mp > 0.f) weigh(std::true_type{});
         else weigh(std::false_type{});
         block_sum(kept_c, kept_w);
         reduce_bins();
@@ -327,7 +326,7 @@ public:
             if (f.count < n) n = f.count, sum = f.weight;
         }
         if (mp > 1.f) kept_c = 1, kept_w = (u64)s.unit;   // nobody reaches it: the first token alone
-        if (floor_units && kept_c < n) n = kept_c, sum = kept_w;
+        if (mp > 0.f && kept_c < n) n = kept_c, sum = kept_w;
         answer(a, r, search(false, pass(u, sum)), n, sum);
     }
 
@@ -393,7 +392,7 @@ private:
         const int more = width == narrow ? 0 : 1;
         return Place{max(bin_of_estimate(v * (1.f - margin)) - more, 0), min(bin_of_estimate(v * (1.f + margin)) + more, kFine - 2)};
     }
-    __device__ bool by_estimate(const SampleArgs& a, int r, int k, float p, float mp, double u, u64 floor_units, bool tiny, double least_u) {
+    __device__ bool by_estimate(const SampleArgs& a, int r, int k, float p, float mp, double u, float least) {
         for (int i = tid; i < kFine; i += kThreads) sh.fine[i] = 0;
         __syncthreads();
         each8([&](const float(&x)[8], int) {
@@ -472,11 +471,11 @@ private:
         if (!places(width)) width = narrow;
         for (; width <= sure; ++width) {
             if (!places(width) && !head) return false;
-            if (collect(a, r, k, p, mp, u, floor_units, tiny, least_u, at, head, at_k, at_p, bk, live)) return true;
+            if (collect(a, r, k, p, mp, u, least, at, head, at_k, at_p, bk, live)) return true;
         }
         return false;
     }
-    __device__ bool collect(const SampleArgs& a, int r, int k, float p, float mp, double u, u64 floor_units, bool tiny, double least_u,
+    __device__ bool collect(const SampleArgs& a, int r, int k, float p, float mp, double u, float least,
                             const Place (&at)[3], bool head, bool at_k, bool at_p, int bk, uint32_t live) {
         // ---- the tokens, and the weights in front of them ----
         u64* list = reinterpret_cast<u64*>(hist);
@@ -518,14 +517,14 @@ private:
                         bump(column, c, units);
                         in |= (uint32_t)(b >= lo0 && b <= (b >= lo2 ? hi2 : b >= lo1 ? hi1 : hi0)) << j;
                         if constexpr (decltype(with_floor)::value) {
-                            const bool keep = x[j] > -INFINITY && (tiny ? ((double)x[j] - s.wide_top) * s.c >= least_u : units >= floor_units);
+                            const bool keep = x[j] > -INFINITY && x[j] >= least;
                             kept_c += keep, kept_w += keep ? units : 0;
                         }
                     }
                     take(x, i, in);
                 });
             };
-            if (floor_units) sum_up(std::true_type{});
+            if (mp > 0.f) sum_up(std::true_type{});
             else sum_up(std::false_type{});
             front[2] = lds64(column);
             front[1] = front[2] + lds64(column + kThreads * 8);
@@ -549,14 +548,14 @@ private:
                 n_list += more;
             }
             __syncthreads();
-            const bool ok = settle(a, r, k, p, mp, u, floor_units, tiny, least_u, at, head, live, at_k, n_list, all_w, front, kept_c, kept_w);
+            const bool ok = settle(a, r, k, p, mp, u, least, at, head, live, at_k, n_list, all_w, front, kept_c, kept_w);
             if (tid < n_ranks) *cluster.map_shared_rank(&sh.done, tid) = ok;
         }
         cluster.sync();
         return sh.done;
     }
     // Rank 0: the searches, over the list.  False where an estimate was too far off.
-    __device__ bool settle(const SampleArgs& a, int r, int k, float p, float mp, double u, u64 floor_units, bool tiny, double least_u,
+    __device__ bool settle(const SampleArgs& a, int r, int k, float p, float mp, double u, float least,
                            const Place (&at)[3], bool head, uint32_t live, bool at_k, int n_list, u64 all_w, const u64 (&front)[3],
                            u64 kept_c, u64 kept_w) {
         u64 n = k > 0 && (uint32_t)k < live ? k : live, sum = all_w;
@@ -572,17 +571,17 @@ private:
         }
         if (mp > 1.f) {
             kept_c = 1, kept_w = (u64)s.unit;   // nobody reaches it: the first token alone
-        } else if (floor_units && head) {   // (what min-p keeps beyond the k-th does not matter)
+        } else if (mp > 0.f && head) {   // (what min-p keeps beyond the k-th does not matter)
             const u64* list = reinterpret_cast<const u64*>(hist);
             kept_c = kept_w = 0;
             for (int i = tid; i < n_list; i += kThreads) {
                 const float x = value_of((uint32_t)(list[i] >> 32));
                 const u64 units = weight_units(s, fmaxf(x, s.low));
-                if (tiny ? ((double)x - s.wide_top) * s.c >= least_u : units >= floor_units) kept_c += 1, kept_w += units;
+                if (x >= least) kept_c += 1, kept_w += units;
             }
             block_sum(kept_c, kept_w);
         }
-        if (floor_units && kept_c < n) n = kept_c, sum = kept_w;
+        if (mp > 0.f && kept_c < n) n = kept_c, sum = kept_w;
         const u64 target = pass(u, sum);
         if (!find_weight(target, at[2], head, front[2], n_list, f)) return false;
         answer(a, r, f, n, sum);
