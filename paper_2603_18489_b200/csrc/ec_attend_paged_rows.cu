@@ -6,7 +6,8 @@
 // that what an unfinished page holds is never multiplied), forms the scores, keeps its own running maximum and sum, and multiplies
 // into its own accumulators.  Nothing but the merge at the end of a unit's keys needs the CTA together.
 //   bf16   mma.sync m16n8k16 (tcgen05 has no shape below 64 rows, and this is far from bound by the tensor pipe: 7.5 % busy), P
-//          rounded to bf16 for the second product as the dense kernels do
+//          rounded to bf16 for the second product as the dense kernels do (outputs are off by 2.1e-3 of their size, 1.7e-3 of it
+//          their own rounding); the sums of the weights are formed from the unrounded ones
 //   fp32   FMA units; a lane has one key and eight rows for the scores, HD / 32 columns of all rows for the output
 // The work is cut as ec_paged.cuh says; attend_paged_combine_kernel joins the units that a cut divided.
 // 32 sequences of 526 to 7892 keys, 32 heads on 8: 94 us, 5.2 TB/s (the bytes alone 76); the rest is planning (3 us), the ends of

@@ -10,6 +10,8 @@
 //   warps 2-17  softmax, four warpgroups: (row tile) x (64-column half); no running maximum in the first pass, a row's
 //               reference is its largest score among the first eight keys of the part that it sees.  They also bring Q into
 //               shared memory (packed rows are rows of several heads and tokens: plain loads, the swizzle by hand)
+// P is rounded to bf16: tcgen05 takes both operands in one type, and a second product for what is left would be half as much work
+// again; sums of the weights are formed from the unrounded ones.  Outputs are off by 2.3e-3 of their size, 1.7e-3 of it their own rounding.
 // The issuer zeroes the rows of the last V tile that stand behind the sequence's end (an unfinished page may hold anything, and
 // 0 x NaN is NaN).  A row sees keys below its limit; a tile whose keys are below the lowest limit of a warp's rows needs no mask.
 // The roles go from unit to unit by themselves: the producer, which is ahead of the others, writes down what the next unit is

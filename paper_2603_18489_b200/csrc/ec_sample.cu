@@ -20,7 +20,7 @@
 //
 // Bound by instructions: some 45 a token for a weight (ten of them 64-bit).  256 x 152064 in bf16, two CTAs a row: 58 % of the issue
 // slots of an SM while it works, 28 % over the launch, which the slowest rows end; the bytes 4 % of the peak.  Of a row without top k on four CTAs (126464 tokens in fp32, clocks): step 1 13 k, counts and places 12 k, weights and
-// taking 20 to 22 k, settling 11 to 20 k; with a top k of 200 48 k in all.  32 rows 38 to 43 us, 256 of 152064 in bf16 210 to 300
+// taking 20 to 22 k, settling 11 to 20 k; with a top k of 200 48 k in all.  32 rows 37 to 43 us, 256 of 152064 in bf16 197 to 300
 // (both by the rows).
 #include "ec_common.cuh"
 #include "ec_tc_ptx.cuh"
